@@ -496,6 +496,80 @@ gnn_status gnn_linear_backward(const void* X, const void* W, const void* dY, int
                                gnn_dtype dtype, void* dX, void* dW, void* ws, size_t ws_bytes,
                                gnn_stream stream);
 
+/* ------------------------------------------------------------------ dense transform per segment */
+
+/* Y[i,:] = act( X[i,:] * W[g(i)] + bias[g(i)] ): the dense transform of a graph with several node types (GNNHeteroGraph of
+ * Sec. 3 "Graph Data Structures"), whose weight depends on the type of the row.  Rows are sorted by type: segment g is rows
+ * seg_ptr[g] .. seg_ptr[g+1]-1, the form that gnn_graph_ptr_from_ids gives (int64 [G+1] on the device, non-decreasing,
+ * 0 <= seg_ptr[0], seg_ptr[G] <= N; read on the device only).  Segments may be empty; rows of no segment (before seg_ptr[0],
+ * from seg_ptr[G] on) become 0.  X [N,K], W [G,K,M], Y [N,M] of dtype, bias float [G,M] or NULL; relu != 0: max(., 0)
+ * before the single rounding (a NaN stays).  K and M: any up to 8192 (fp32: 2048; GNN_ERR_UNSUPPORTED beyond), G K < 2^31.
+ * Matrices and ws are 16-byte aligned.  Tensor cores with fp32 accumulation: bf16 directly, fp32 by an exact three-term bf16
+ * split as in gnn_linear (a value that is not finite gives NaN in the results it enters).
+ * Rows of one segment only ever meet their own weight: what another segment holds (infinities, NaN) does not reach them.
+ * ws: gnn_linear_segments_workspace(..., backward = 0) bytes, asked for the sizes of each call; it holds copies of bf16
+ * matrices whose rows do not start on 16 bytes and the terms of fp32 ones.  Its first 4 bytes are the status word of
+ * gnn_linear. */
+size_t gnn_linear_segments_workspace(int32_t N, int G, int K, int M, gnn_dtype dtype, int backward);
+gnn_status gnn_linear_segments(const void* X, const int64_t* seg_ptr, const void* W, int32_t N, int G, int K, int M,
+                               gnn_dtype dtype, const float* bias, int relu, void* Y, void* ws, size_t ws_bytes,
+                               gnn_stream stream);
+
+/* dX[i,:] = dY[i,:] * W[g(i)]^T (0 for a row of no segment) and dW[g] = X_g^T * dY_g ([G,K,M] of dtype, 0 for an empty
+ * segment); either output may be NULL.  X is needed only for dW, W only for dX.  bias / relu: gnn_row_epilogue_backward gives
+ * dZ, gnn_reduce_nodes(seg_ptr, ..., GNN_SUM, dZ) the gradient of bias.  Sums over the rows run in a fixed order.
+ * ws: gnn_linear_segments_workspace(..., backward = 1) bytes. */
+gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, const void* W, const void* dY, int32_t N,
+                                        int G, int K, int M, gnn_dtype dtype, void* dX, void* dW, void* ws,
+                                        size_t ws_bytes, gnn_stream stream);
+
+/* ------------------------------------------------------------------ dense transform in 8 bits */
+
+/* Rows to 8 bits: scale[i] = max_k |X[i,k]| / 127 (fp32, one rounding), q[i,k] = X[i,k] / scale[i] rounded to the nearest
+ * integer, ties to even, as the exact quotient would be.  A row of zeros has scale 0 and zeros; a row with a value that is
+ * not finite has scale NaN and zeros, so that what is computed from it is NaN.  X [N,K] of dtype, q int8 [N,K] (both
+ * 16-byte aligned), scale float [N].  Weights [K,M] are transposed first: a row of q is an output channel. */
+gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, int8_t* q, float* scale, gnn_stream stream);
+
+/* Y[i,m] = act( x_scale[i] * w_scale[m] * sum_k xq[i,k] * wq[m,k] + bias[m] ): gnn_linear_bias_act for answering, with
+ * features and weights in 8 bits.  xq int8 [N,K], wq int8 [M,K] (a row per output channel), both 16-byte aligned, x_scale
+ * float [N], w_scale float [M], bias float [M] or NULL, Y [N,M] of dtype, 16-byte aligned.  The sums are exact (int32; K up
+ * to 131071, GNN_ERR_UNSUPPORTED beyond); scales, bias and relu in fp32, one rounding to dtype.
+ * ws: gnn_linear_i8_workspace(N, K, M) bytes, asked for the sizes of each call, 16-byte aligned; its first 4 bytes are the
+ * status word of gnn_linear. */
+size_t gnn_linear_i8_workspace(int32_t N, int K, int M);
+gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* wq, const float* w_scale, int32_t N, int K,
+                         int M, gnn_dtype dtype, const float* bias, int relu, void* Y, void* ws, size_t ws_bytes,
+                         gnn_stream stream);
+
+/* ------------------------------------------------------------------ log probabilities of classes */
+
+/* What the scores of a node classifier (the last Dense layer of the training example) or of a ranking of entities answer,
+ * in one pass.  Z [N,C] of dtype, 16-byte aligned, contiguous; per row, with p = softmax(z):
+ *   lse      float [N]      log sum_c exp z_c
+ *   logp     float [N]      z[label] - lse; 0 where label (int32 [N]) is outside 0 .. C-1, say -1 for an unlabelled node
+ *   entropy  float [N]      -sum_c p_c log p_c
+ *   top_idx  int32 [N,top], top_logp float [N,top]   the `top` classes of largest score, best first, the lower index first
+ *                           among equals (+0 and -0 are equal), and their log probabilities; top up to min(C, 32)
+ * logp, entropy and lse may each be NULL (label too, without logp).  Math in fp32; bf16 scores are exact inputs.  The
+ * largest score's own term is kept apart from the sum, so that a nearly sure row keeps the digits of its log probability.
+ * A class at -inf is masked: p = 0.  A row of nothing else: lse, logp of its label and top_logp -inf, entropy 0.  A NaN or
+ * +inf makes the row's results NaN; its top_idx are still classes of the row (a NaN is the worst of them).
+ * ws: gnn_log_probs_workspace bytes (0 where rows are not divided), 16-byte aligned. */
+size_t gnn_log_probs_workspace(int32_t N, int C, int top, gnn_dtype dtype);
+gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, gnn_dtype dtype, int top, float* logp,
+                         float* entropy, float* lse, float* top_logp, int32_t* top_idx, void* ws, size_t ws_bytes,
+                         gnn_stream stream);
+
+/* dZ[i,c] = dlogp[i] ([c = label[i]] - p_c) - dentropy[i] p_c (log p_c + entropy[i]) with p_c = exp(Z[i,c] - lse[i]), of dtype.
+ * lse and entropy are gnn_log_probs' outputs.  dlogp (float [N], needs label) and dentropy (float [N], needs entropy) may be
+ * NULL; dlogp of a row without a label is not used.  A class at -inf gets 0 (its label's share excepted); a row whose
+ * lse is under -1e30 (all classes at -inf, or at the type's lowest value) zeros.  dZ may be Z.
+ * The listed best classes are not differentiated. */
+gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const float* lse, const float* entropy,
+                                  const float* dlogp, const float* dentropy, int32_t N, int C, gnn_dtype dtype, void* dZ,
+                                  gnn_stream stream);
+
 /* ------------------------------------------------------------------ aggregate -> transform fusion */
 
 /* Y = act( (op over p in row i of w[p] * X[col[p],:]) * W + bias ): the fused propagate followed by the

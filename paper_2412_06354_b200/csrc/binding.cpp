@@ -881,6 +881,178 @@ FN(propagate_linear_backward) {
     return wrap_all(dX, dW);
 }
 
+// ---------------------------------------------------------------- typed, 8-bit and last layers
+// These calls run on the device of their tensors, whichever is current, on that device's current stream; all tensors lie there.
+struct OnDevice {
+    c10::cuda::CUDAGuard guard;
+    c10::Device dev;
+    explicit OnDevice(const at::Tensor& x) : guard(x.device()), dev(x.device()) {}
+    void same(const at::Tensor& t, const char* name) const {
+        if (t.defined() && t.device() != dev) raise(PyExc_ValueError, std::string(name) + " lies on another device");
+    }
+};
+static void shaped(const at::Tensor& t, at::IntArrayRef shape, const char* name) {
+    if (t.defined() && t.sizes() != shape) raise(PyExc_ValueError, std::string(name) + " has another shape than the other arguments ask for");
+}
+static void dims(const at::Tensor& t, int64_t n, const char* name) {
+    if (t.dim() != n) raise(PyExc_ValueError, std::string(name) + " must have " + std::to_string(n) + " dimensions");
+}
+static void same_type(const at::Tensor& t, const at::Tensor& x, const char* name) {
+    if (t.defined() && t.scalar_type() != x.scalar_type()) raise(PyExc_TypeError, std::string(name) + " must have the type of the features");
+}
+static int32_t rows32(int64_t n) {
+    if (n > INT32_MAX) raise(PyExc_ValueError, "too many rows");
+    return (int32_t)n;
+}
+static int size32(int64_t n) {
+    if (n > INT32_MAX) raise(PyExc_ValueError, "too large");
+    return (int)n;
+}
+static const int8_t* bytes8(const at::Tensor& t, const char* name) {
+    if (t.scalar_type() != at::kChar) raise(PyExc_TypeError, std::string(name) + " must be torch.int8, got " + c10::toString(t.scalar_type()));
+    return (const int8_t*)t.data_ptr();
+}
+// a caller's workspace: bytes, on the device, contiguous
+static void workspace_ok(const at::Tensor& t, const OnDevice& on) {
+    if (!t.defined()) return;
+    on.same(t, "ws");
+    if (t.element_size() != 1 || !t.is_contiguous()) raise(PyExc_TypeError, "ws must be a contiguous tensor of bytes");
+}
+
+// (X, seg_ptr, W, bias, relu, ws, return_ws) -> Y or (Y, ws)
+FN(linear_segments) {
+    const at::Tensor &X = A.dev(0), &sp = A.dev(1), &W = A.dev(2), &bias = A.t(3);
+    const OnDevice on(X);
+    dims(X, 2, "X"); dims(W, 3, "W"); dims(sp, 1, "seg_ptr");
+    const int64_t N = X.size(0), K = X.size(1), G = W.size(0), M = W.size(2);
+    shaped(W, {G, K, M}, "W"); shaped(sp, {G + 1}, "seg_ptr"); shaped(bias, {G, M}, "bias");
+    same_type(W, X, "W");
+    on.same(sp, "seg_ptr"); on.same(W, "W"); on.same(bias, "bias"); workspace_ok(A.t(5), on);
+    const int relu = A.flag(4);
+    const bool wanted = A.flag(6);
+    const gnn_dtype dt = dtype_of(X);
+    const int32_t n = rows32(N);
+    const int g = size32(G), k = size32(K), m = size32(M);
+    const int64_t* ptrs = i64(sp, "seg_ptr");
+    const float* b = f32(bias, "bias");
+    at::Tensor Y = empty({N, M}, X.scalar_type(), X.device());
+    const size_t need = gnn_linear_segments_workspace(n, g, k, m, dt, 0);
+    const at::Tensor wt = linear_scratch(A, 5, wanted, need, X.device());
+    Scratch ws(wt, need, X.device());
+    const gnn_stream st = stream();
+    CALL(gnn_linear_segments(ptr(X), ptrs, ptr(W), n, g, k, m, dt, b, relu, ptr(Y), ws.p, ws.n, st));
+    return wanted ? wrap_all(Y, wt) : wrap(Y);
+}
+
+// (X, seg_ptr, W, dY, want_dX, want_dW, ws, return_ws) -> (dX, dW) or (dX, dW, ws)
+FN(linear_segments_backward) {
+    const bool want_dX = A.flag(4), want_dW = A.flag(5), wanted = A.flag(7);
+    const at::Tensor &sp = A.dev(1), &W = A.dev(2), &dY = A.dev(3), &X = want_dW ? A.dev(0) : A.t(0);
+    const OnDevice on(dY);
+    dims(dY, 2, "dY"); dims(W, 3, "W"); dims(sp, 1, "seg_ptr");
+    const int64_t N = dY.size(0), M = dY.size(1), G = W.size(0), K = W.size(1);
+    shaped(W, {G, K, M}, "W"); shaped(sp, {G + 1}, "seg_ptr"); shaped(X, {N, K}, "X");
+    same_type(W, dY, "W"); same_type(X, dY, "X");
+    on.same(sp, "seg_ptr"); on.same(W, "W"); on.same(X, "X"); workspace_ok(A.t(6), on);
+    const gnn_dtype dt = dtype_of(dY);
+    const int32_t n = rows32(N);
+    const int g = size32(G), k = size32(K), m = size32(M);
+    const int64_t* ptrs = i64(sp, "seg_ptr");
+    at::Tensor dX, dW;
+    if (want_dX) dX = empty({N, K}, dY.scalar_type(), dY.device());
+    if (want_dW) dW = empty({G, K, M}, dY.scalar_type(), dY.device());
+    const size_t need = gnn_linear_segments_workspace(n, g, k, m, dt, 1);
+    const at::Tensor wt = linear_scratch(A, 6, wanted, need, dY.device());
+    Scratch ws(wt, need, dY.device());
+    const gnn_stream st = stream();
+    CALL(gnn_linear_segments_backward(ptr(X), ptrs, ptr(W), ptr(dY), n, g, k, m, dt, ptr(dX), ptr(dW), ws.p, ws.n, st));
+    return wanted ? wrap_all(dX, dW, wt) : wrap_all(dX, dW);
+}
+
+// (X) -> (q, scale)
+FN(quantize_rows) {
+    const at::Tensor& X = A.dev(0);
+    const OnDevice on(X);
+    dims(X, 2, "X");
+    const int64_t N = X.size(0), K = X.size(1);
+    const gnn_dtype dt = dtype_of(X);
+    const int32_t n = rows32(N);
+    const int k = size32(K);
+    at::Tensor q = empty({N, K}, at::kChar, X.device()), scale = empty({N}, at::kFloat, X.device());
+    const gnn_stream st = stream();
+    CALL(gnn_quantize_rows(ptr(X), n, k, dt, (int8_t*)ptr(q), (float*)ptr(scale), st));
+    return wrap_all(q, scale);
+}
+
+// (xq, x_scale, wq, w_scale, bias, relu, bf16, ws, return_ws) -> Y or (Y, ws)
+FN(linear_i8) {
+    const at::Tensor &xq = A.dev(0), &xs = A.dev(1), &wq = A.dev(2), &wsc = A.dev(3), &bias = A.t(4);
+    const OnDevice on(xq);
+    dims(xq, 2, "xq"); dims(wq, 2, "wq");
+    const int64_t N = xq.size(0), K = xq.size(1), M = wq.size(0);
+    shaped(wq, {M, K}, "wq"); shaped(xs, {N}, "x_scale"); shaped(wsc, {M}, "w_scale"); shaped(bias, {M}, "bias");
+    on.same(xs, "x_scale"); on.same(wq, "wq"); on.same(wsc, "w_scale"); on.same(bias, "bias"); workspace_ok(A.t(7), on);
+    const int relu = A.flag(5);
+    const gnn_dtype dt = A.flag(6) ? GNN_BF16 : GNN_F32;
+    const bool wanted = A.flag(8);
+    const int32_t n = rows32(N);
+    const int k = size32(K), m = size32(M);
+    const int8_t *x8 = bytes8(xq, "xq"), *w8 = bytes8(wq, "wq");
+    const float *sx = f32(xs, "x_scale"), *sw = f32(wsc, "w_scale"), *b = f32(bias, "bias");
+    at::Tensor Y = empty({N, M}, dt == GNN_BF16 ? at::kBFloat16 : at::kFloat, xq.device());
+    const size_t need = gnn_linear_i8_workspace(n, k, m);
+    const at::Tensor wt = linear_scratch(A, 7, wanted, need, xq.device());
+    Scratch ws(wt, need, xq.device());
+    const gnn_stream st = stream();
+    CALL(gnn_linear_i8(x8, sx, w8, sw, n, k, m, dt, b, relu, ptr(Y), ws.p, ws.n, st));
+    return wanted ? wrap_all(Y, wt) : wrap(Y);
+}
+
+// (Z, label, top, want_entropy, ws) -> (logp, entropy, lse, top_logp, top_idx)
+FN(log_probs) {
+    const at::Tensor &Z = A.dev(0), &label = A.t(1);
+    const OnDevice on(Z);
+    dims(Z, 2, "Z");
+    const int64_t N = Z.size(0), C = Z.size(1), top = A.i(2);
+    shaped(label, {N}, "label");
+    on.same(label, "label"); workspace_ok(A.t(4), on);
+    const gnn_dtype dt = dtype_of(Z);
+    const int32_t n = rows32(N);
+    const int c = size32(C);
+    if (top < 0 || top > C) raise(PyExc_ValueError, "top must lie between 0 and the number of classes");
+    const int32_t* y = i32(label, "label");
+    at::Tensor logp, entropy, lse = empty({N}, at::kFloat, Z.device());
+    if (label.defined()) logp = empty({N}, at::kFloat, Z.device());
+    if (A.flag(3)) entropy = empty({N}, at::kFloat, Z.device());
+    at::Tensor tl = empty({N, top}, at::kFloat, Z.device()), ti = empty({N, top}, at::kInt, Z.device());
+    const size_t need = gnn_log_probs_workspace(n, c, (int)top, dt);
+    Scratch ws(A.t(4), need, Z.device());
+    const gnn_stream st = stream();
+    CALL(gnn_log_probs(ptr(Z), y, n, c, dt, (int)top, (float*)ptr(logp), (float*)ptr(entropy), (float*)ptr(lse), (float*)ptr(tl), (int32_t*)ptr(ti), ws.p, ws.n, st));
+    return wrap_all(logp, entropy, lse, tl, ti);
+}
+
+// (Z, label, lse, dlogp, entropy, dentropy) -> dZ
+FN(log_probs_backward) {
+    const at::Tensor &Z = A.dev(0), &label = A.t(1), &lse = A.dev(2), &dlogp = A.t(3), &entropy = A.t(4), &dentropy = A.t(5);
+    const OnDevice on(Z);
+    dims(Z, 2, "Z");
+    const int64_t N = Z.size(0), C = Z.size(1);
+    for (const auto& [t, name] : {std::pair<const at::Tensor*, const char*>{&label, "label"}, {&lse, "lse"}, {&dlogp, "dlogp"}, {&entropy, "entropy"}, {&dentropy, "dentropy"}}) {
+        shaped(*t, {N}, name);
+        on.same(*t, name);
+    }
+    const gnn_dtype dt = dtype_of(Z);
+    const int32_t n = rows32(N);
+    const int c = size32(C);
+    const int32_t* y = i32(label, "label");
+    const float *l = f32(lse, "lse"), *g = f32(dlogp, "dlogp"), *H = f32(entropy, "entropy"), *h = f32(dentropy, "dentropy");
+    at::Tensor dZ = empty_like(Z);
+    const gnn_stream st = stream();
+    CALL(gnn_log_probs_backward(ptr(Z), y, l, H, g, h, n, c, dt, ptr(dZ), st));
+    return wrap(dZ);
+}
+
 // (module dict, real torch, error class): what the calls take from the Python module
 FN(attach) {
     g_module_dict = A.at(0);
@@ -900,6 +1072,7 @@ PyMethodDef methods[] = {
     ENTRY(gatv2_logits), ENTRY(gatv2_logits_backward), ENTRY(gather), ENTRY(gather_backward), ENTRY(apply_edges), ENTRY(aggregate),
     ENTRY(aggregate_backward), ENTRY(edge_softmax), ENTRY(edge_softmax_backward), ENTRY(axpby), ENTRY(reduce_nodes), ENTRY(reduce_nodes_backward),
     ENTRY(gat_fused), ENTRY(gat_fused_backward), ENTRY(linear), ENTRY(linear_backward), ENTRY(propagate_linear), ENTRY(propagate_linear_backward),
+    ENTRY(linear_segments), ENTRY(linear_segments_backward), ENTRY(quantize_rows), ENTRY(linear_i8), ENTRY(log_probs), ENTRY(log_probs_backward),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "calls of the C ABI on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};

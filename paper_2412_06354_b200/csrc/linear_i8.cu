@@ -1,0 +1,282 @@
+// Dense transform in 8-bit integers, for answering: rows and output channels carry a scale each,
+//   Y[i,m] = act(sx[i] * sw[m] * sum_k xq[i,k] * wq[m,k] + bias[m]),
+// and the rounding of rows to 8 bits that makes the operands.  The sums are exact (int32); the products run on the tensor
+// cores through the pipeline of segment_gemm.cuh, a few rows on four-product integer instructions.
+#include "segment_gemm.cuh"
+
+namespace gnn {
+
+constexpr int I8_SLOT = 54;  // of allow_big_smem: two of them
+
+// ------------------------------------------------------------------ rows to 8 bits
+// scale = max |x| / 127, q = x / scale rounded to the nearest integer, ties to even, as the exact quotient would be: the
+// estimate x * (1 / scale) is off by less than 1e-4, and what remains, x - q * scale, is exact in fp32 (a multiple of the
+// last bit of scale, or of half of it where q is 1, and at most about half of scale), so one comparison with scale / 2 finds
+// the neighbour where the estimate fell on the wrong side.
+__device__ __forceinline__ int round_quotient(float x, float inv, float scale) {
+    float q = rintf(x * inv);
+    const float r = 2.f * fmaf(-q, scale, x);
+    const float a = fabsf(r);
+    if (a >= scale) {  // rare
+        const bool odd = ((int)q & 1) != 0;
+        if (a > scale || odd) q += r > 0.f ? 1.f : -1.f;
+    }
+    return (int)q;
+}
+
+struct RowScale {
+    float scale, inv, s, up;
+    // from the bits of max |x|: not finite -> scale NaN and zeros; scale 0 (or underflown to it) -> zeros
+    __device__ __forceinline__ explicit RowScale(uint32_t top) {
+        scale = top < 0x7F800000u ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7FC00000u);
+        // 1 / scale would overflow: the same quotient of values 2^80 times as large (exact)
+        up = scale < 1e-30f ? 1.2089258196146292e24f : 1.f;
+        s = scale * up;
+        inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;  // NaN and 0: all zeros
+        if (!(s > 0.f)) up = 0.f;
+    }
+    __device__ __forceinline__ int operator()(float x) const { return up == 0.f ? 0 : round_quotient(x * up, inv, s); }
+};
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+template <typename T>
+__device__ __forceinline__ uint32_t chunk_top(uint4 v) {
+    float f[Chunk<T>::N];
+    Chunk<T>::unpack(v, f);
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < Chunk<T>::N; ++k) m = max(m, abs_bits(f[k]));
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ void chunk_out(uint4 v, const RowScale& rs, int8_t* q) {
+    float f[Chunk<T>::N];
+    Chunk<T>::unpack(v, f);
+    uint32_t w[Chunk<T>::N / 4];
+#pragma unroll
+    for (int k = 0; k < Chunk<T>::N / 4; ++k)
+        w[k] = (uint32_t)(rs(f[4 * k]) & 0xFF) | (uint32_t)(rs(f[4 * k + 1]) & 0xFF) << 8 | (uint32_t)(rs(f[4 * k + 2]) & 0xFF) << 16 | (uint32_t)(rs(f[4 * k + 3]) & 0xFF) << 24;
+    if constexpr (Chunk<T>::N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(q) = w[0];
+}
+
+// L lanes per row of whole 16-byte chunks, up to CH chunks per lane held in registers between the two passes
+template <typename T, int L, int CH>
+__global__ void __launch_bounds__(256)
+quantize_rows_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
+    pdl_wait();
+    constexpr int PER = Chunk<T>::N;
+    const int64_t row = (blockIdx.x * (int64_t)256 + threadIdx.x) / L;
+    const int lane = threadIdx.x % L, chunks = K / PER;
+    const bool on = row < N;
+    const T* const x = X + row * K;
+    uint4 v[CH];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        v[c] = make_uint4(0, 0, 0, 0);
+        if (on && lane + c * L < chunks) v[c] = ld_16(x + (lane + c * L) * PER);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) top = max(top, chunk_top<T>(v[c]));
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (!on) return;
+    const RowScale rs(top);
+    if (lane == 0) scale[row] = rs.scale;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+        if (lane + c * L < chunks) chunk_out<T>(v[c], rs, q + row * K + (lane + c * L) * PER);
+}
+
+// any K: a block per row, elements one by one, read twice
+template <typename T>
+__global__ void __launch_bounds__(256)
+quantize_any_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
+    pdl_wait();
+    __shared__ uint32_t tops[8];
+    for (int64_t row = blockIdx.x; row < N; row += gridDim.x) {
+        const T* const x = X + row * K;
+        uint32_t top = 0;
+        for (int k = threadIdx.x; k < K; k += 256) top = max(top, abs_bits((float)x[k]));
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = max(top, tops[w]);
+        __syncthreads();
+        const RowScale rs(top);
+        if (threadIdx.x == 0) scale[row] = rs.scale;
+        for (int k = threadIdx.x; k < K; k += 256) q[row * K + k] = (int8_t)rs((float)x[k]);
+    }
+}
+
+template <typename T>
+static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scale, cudaStream_t st) {
+    constexpr int PER = Chunk<T>::N;
+    const int chunks = K / PER;
+    auto run = [&](auto kernel, int lanes) { launch_overlapped(kernel, dim3((unsigned)ceil_div(N * lanes, 256)), dim3(256), 0, st, X, N, K, q, scale); };
+    if (K % PER != 0 || chunks > 256) {
+        launch_overlapped(quantize_any_kernel<T>, dim3((unsigned)(N < 148 * 8 ? N : 148 * 8)), dim3(256), 0, st, X, N, K, q, scale);
+        return;
+    }
+    if (chunks <= 4) run(quantize_rows_kernel<T, 4, 1>, 4);
+    else if (chunks <= 8) run(quantize_rows_kernel<T, 4, 2>, 4);
+    else if (chunks <= 16) run(quantize_rows_kernel<T, 8, 2>, 8);
+    else if (chunks <= 32) run(quantize_rows_kernel<T, 16, 2>, 16);
+    else if (chunks <= 64) run(quantize_rows_kernel<T, 32, 2>, 32);
+    else if (chunks <= 128) run(quantize_rows_kernel<T, 32, 4>, 32);
+    else run(quantize_rows_kernel<T, 32, 8>, 32);
+}
+
+// ------------------------------------------------------------------ the product
+// A few rows: a warp per output channel and four rows, four products to an instruction.  Bound by reading the weights once.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256)
+linear_i8_rows_kernel(const int8_t* xq, const float* sx, const int8_t* wq, const float* sw, int N, int K, int M, const float* bias, int relu, T* __restrict__ Y, int* status) {
+    pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *status = 0;
+    constexpr int R = 4;
+    const int lane = threadIdx.x & 31, m = (int)blockIdx.x * 8 + (int)(threadIdx.x >> 5), n0 = (int)blockIdx.y * R;
+    if (m >= M) return;
+    const int8_t* const w = wq + (int64_t)m * K;
+    int acc[R] = {0, 0, 0, 0};
+    if constexpr (WIDE) {
+#pragma unroll 2
+        for (int k = lane * 16; k < K; k += 512) {
+            const uint4 a = ld_16(w + k);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (n0 + r >= N) break;
+                const uint4 b = ld_16(xq + (int64_t)(n0 + r) * K + k);
+                acc[r] = __dp4a((int)a.x, (int)b.x, acc[r]);
+                acc[r] = __dp4a((int)a.y, (int)b.y, acc[r]);
+                acc[r] = __dp4a((int)a.z, (int)b.z, acc[r]);
+                acc[r] = __dp4a((int)a.w, (int)b.w, acc[r]);
+            }
+        }
+    } else {
+        for (int k = lane; k < K; k += 32) {
+            const int a = w[k];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (n0 + r < N) acc[r] += a * xq[(int64_t)(n0 + r) * K + k];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = __reduce_add_sync(0xFFFFFFFFu, acc[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (lane != r || n0 + r >= N) continue;
+        float y = (float)acc[r] * (sx[n0 + r] * sw[m]);
+        if (bias) y += bias[m];
+        if (relu) y = y < 0.f ? 0.f : y;
+        Y[(int64_t)(n0 + r) * M + m] = T(y);
+    }
+}
+
+// rows of bytes on 16-byte starts, zeros behind the last
+__global__ void __launch_bounds__(256)
+pad_bytes_kernel(const int8_t* src, int64_t rows, int cols, int8_t* __restrict__ dst, int ld) {
+    pdl_wait();
+    const int chunks = ld / 16;
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= rows * chunks) return;
+    const int64_t r = i / chunks;
+    const int c = (int)(i - r * chunks) * 16;
+    union { int8_t b[16]; uint4 v; } u;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) u.b[k] = c + k < cols ? src[r * cols + c + k] : (int8_t)0;
+    *reinterpret_cast<uint4*>(dst + r * ld + c) = u.v;
+}
+
+static int up16(int x) { return (x + 15) & ~15; }
+static bool i8_few_rows(int32_t N) { return N <= 8; }
+
+struct I8Ws {
+    size_t x, w, bytes;
+    I8Ws(int64_t N, int K, int M) {
+        const bool pads = K % 16 != 0 && !i8_few_rows((int32_t)N);
+        x = 256;
+        w = x + (pads ? up256((size_t)N * up16(K)) : 0);
+        bytes = w + (pads ? up256((size_t)M * up16(K)) : 0);
+    }
+};
+
+static const int8_t* padded_bytes(const int8_t* src, int64_t rows, int cols, void* dst, cudaStream_t st) {
+    const int ld = up16(cols);
+    if (ld == cols) return src;
+    launch_overlapped(pad_bytes_kernel, dim3((unsigned)ceil_div(rows * (ld / 16), 256)), dim3(256), 0, st, src, rows, cols, (int8_t*)dst, ld);
+    return (const int8_t*)dst;
+}
+
+}  // namespace gnn
+
+using namespace gnn;
+
+extern "C" {
+
+gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, int8_t* q, float* scale, gnn_stream stream) {
+    const char* who = "gnn_quantize_rows";
+    GNN_REQUIRE(N >= 0 && K > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
+    GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (N == 0) return GNN_OK;
+    GNN_REQUIRE(X && q && scale, GNN_ERR_INVALID_ARG, "%s: null argument", who);
+    GNN_REQUIRE(aligned16(X) && aligned16(q), GNN_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
+    if (dtype == GNN_F32) launch_quantize((const float*)X, N, K, q, scale, as_stream(stream));
+    else launch_quantize((const __nv_bfloat16*)X, N, K, q, scale, as_stream(stream));
+    GNN_CHECK_LAUNCH(who);
+    return GNN_OK;
+}
+
+size_t gnn_linear_i8_workspace(int32_t N, int K, int M) {
+    if (N < 0 || K <= 0 || M <= 0) return 0;
+    return I8Ws(N, K, M).bytes;
+}
+
+gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* wq, const float* w_scale, int32_t N, int K, int M, gnn_dtype dtype,
+                         const float* bias, int relu, void* Y, void* ws, size_t ws_bytes, gnn_stream stream) {
+    const char* who = "gnn_linear_i8";
+    GNN_REQUIRE(N >= 0 && K > 0 && M > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
+    GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
+    // 128 * 128 * K stays inside int32
+    GNN_REQUIRE(K <= 131071 && N < INT32_MAX - TC_ROWS, GNN_ERR_UNSUPPORTED, "%s: K up to 131071", who);
+    const I8Ws iw(N, K, M);
+    GNN_REQUIRE(ws && ws_bytes >= iw.bytes, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed", who, iw.bytes);
+    cudaStream_t st = as_stream(stream);
+    const bool few = i8_few_rows(N);
+    if (N == 0) return GNN_OK;
+    GNN_REQUIRE(xq && x_scale && wq && w_scale && Y, GNN_ERR_INVALID_ARG, "%s: null argument", who);
+    GNN_REQUIRE(aligned16(xq) && aligned16(wq) && aligned16(Y) && aligned16(ws), GNN_ERR_INVALID_ARG, "%s: matrices and workspace must be 16-byte aligned", who);
+    if (few) {
+        const dim3 grid((unsigned)ceil_div(M, 8), (unsigned)ceil_div(N, 4));
+        auto run = [&](auto kernel, auto* y) { launch_overlapped(kernel, grid, dim3(256), 0, st, xq, x_scale, wq, w_scale, (int)N, K, M, bias, relu, y, (int*)ws); };
+        if (dtype == GNN_F32) K % 16 == 0 ? run(linear_i8_rows_kernel<float, true>, (float*)Y) : run(linear_i8_rows_kernel<float, false>, (float*)Y);
+        else K % 16 == 0 ? run(linear_i8_rows_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)Y) : run(linear_i8_rows_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)Y);
+        GNN_CHECK_LAUNCH(who);
+        return GNN_OK;
+    }
+    GNN_REQUIRE(tensor_map_encoder_available(), GNN_ERR_CUDA, "%s: the driver has no tensor-map encoder", who);
+    const int8_t* const xp = padded_bytes(xq, N, K, (char*)ws + iw.x, st);
+    const int8_t* const wp = padded_bytes(wq, M, K, (char*)ws + iw.w, st);
+    GNN_CHECK_LAUNCH(who);
+    SegGemmParams P = {};
+    const int64_t row_tiles = ceil_div(N, TC_ROWS);
+    P.seg_ptr = nullptr; P.G = 1; P.N = N;
+    P.bn = sg_block(M, 256, row_tiles);
+    P.tiles_n = (M + P.bn - 1) / P.bn; P.tiles_m = 1;
+    P.units = row_tiles * P.tiles_n;
+    P.slices = (K + 127) / 128;
+    P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
+    P.rows_out = TC_ROWS; P.cols_out = M;
+    P.out = Y; P.vec = (size_t)M * elem_size(dtype) % 16 == 0;
+    P.bias = bias; P.relu = relu; P.sx = x_scale; P.sw = w_scale;
+    P.status = (int*)ws; P.reset = 1;
+    CUtensorMap mapA, mapB;
+    if (!make_map_planes(&mapA, xp, true, 1, N, K, up16(K), P.a_rows) || !make_map_planes(&mapB, wp, true, 1, M, K, up16(K), P.bn))
+        GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
+    return dtype == GNN_F32 ? sg_launch<SG_I8, 1, float>(who, I8_SLOT, mapA, mapB, P, st) : sg_launch<SG_I8, 1, __nv_bfloat16>(who, I8_SLOT + 1, mapA, mapB, P, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,258 @@
+// Dense transform whose weight depends on the row's segment (the node types or relations of a heterogeneous graph):
+//   Y[i,:] = act(X[i,:] * W[g(i)] + bias[g(i)]),  dX[i,:] = dY[i,:] * W[g(i)]^T,  dW[g] = X_g^T * dY_g
+// Entry points, their workspaces and the small kernels around the products of segment_gemm.cuh: padded copies of bf16 matrices
+// whose rows do not start on 16 bytes, the three bf16 terms of fp32 matrices, the ordered sum of dW's partials.
+#include "segment_gemm.cuh"
+
+namespace gnn {
+
+constexpr int LS_SLOT = 48;  // of allow_big_smem: six of them
+
+// Rows of fp32 as three planes of bf16 rows (x = x1 + x2 + x3 exactly), or bf16 rows on 16-byte starts (one plane): a thread
+// writes 8 elements of each plane.  Rows of dst are ld elements apart; what follows the last column is zero.
+template <typename T>
+__global__ void __launch_bounds__(256)
+split_rows_kernel(const T* src, int64_t rows, int cols, __nv_bfloat16* __restrict__ dst, int ld, int vec) {
+    pdl_wait();
+    const int chunks = ld / 8;
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= rows * chunks) return;
+    const int64_t r = i / chunks;
+    const int c = (int)(i - r * chunks) * 8;
+    float x[8];
+    const T* const p = src + r * cols + c;
+    if (vec && c + 8 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            Chunk<float>::unpack(ld_16(p), x);
+            Chunk<float>::unpack(ld_16(p + 4), x + 4);
+        } else {
+            Chunk<__nv_bfloat16>::unpack(ld_16(p), x);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = c + k < cols ? (float)p[k] : 0.f;
+    }
+#pragma unroll
+    for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+        const uint4 v = Chunk<__nv_bfloat16>::pack(x);
+        *reinterpret_cast<uint4*>(dst + (l * rows + r) * (int64_t)ld + c) = v;
+        float t[8];
+        Chunk<__nv_bfloat16>::unpack(v, t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] -= t[k];  // exact: the rounded term shares the leading bits
+    }
+}
+
+// dW of the segments that more than one part holds (their partials in ascending order) or none (zeros).  A block of 256
+// threads per 1024 elements of a segment.
+template <typename T>
+__global__ void __launch_bounds__(256)
+segment_sum_kernel(const int64_t* seg_ptr, int G, int64_t N, int64_t part_rows, const float* part, int64_t size, T* __restrict__ dW) {
+    pdl_wait();
+    for (int g = blockIdx.y; g < G; g += gridDim.y) {
+        int64_t a = seg_ptr[g], b = seg_ptr[g + 1];
+        a = a < 0 ? 0 : a > N ? N : a;
+        b = b < 0 ? 0 : b > N ? N : b;
+        const int64_t first = a / part_rows, last = (b - 1) / part_rows;
+        if (b > a && first == last) continue;  // written by the product
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t e = blockIdx.x * (int64_t)1024 + k * 256 + threadIdx.x;
+            if (e >= size) break;
+            float s = 0.f;
+            if (b > a) {
+                // the first part holds the segment's start (cut at the part's end: odd), the others begin inside it (even)
+                s = part[(2 * first + (a >= first * part_rows ? 1 : 0)) * size + e];
+#pragma unroll 4
+                for (int64_t p = first + 1; p <= last; ++p) s += part[2 * p * size + e];
+            }
+            dW[g * size + e] = T(s);
+        }
+    }
+}
+
+static int up8(int x) { return (x + 7) & ~7; }
+
+// How the rows are cut for dW: parts x tiles blocks of work on 148 SMs.  Few parts mean few partials; as many as keep the SMs
+// busy: the smallest number whose last wave costs at most 5 % over the best of all numbers, parts of at least 256 rows.  And of
+// at most 4096 (bf16: 65536) rows: every 16 rows the accumulator loses up to one unit of its 24th bit, so that a sum of terms
+// of one sign is off by 4096 / 16 * 2^-24 = 1.5e-5 of its value at most, half that on average (bf16: 2^-12, under the rounding).
+static int64_t dw_parts(int64_t N, int64_t tiles, bool f32) {
+    const int64_t longest = f32 ? 4096 : 65536, least = N > longest ? ceil_div(N, longest) : 1;
+    int64_t most = N / 256;
+    if (most > 296) most = 296;
+    if (most < least) most = least;
+    auto cost = [&](int64_t p) { return (double)ceil_div(p * tiles, 148) / (double)p; };
+    double best = cost(least);
+    for (int64_t p = least + 1; p <= most; ++p) best = cost(p) < best ? cost(p) : best;
+    for (int64_t p = least; p <= most; ++p)
+        if (cost(p) <= 1.05 * best) return p;
+    return least;
+}
+
+struct SegWs {
+    size_t x, dy, w, part, bytes;
+    int64_t parts;
+    int bn, tiles_n, tiles_m;
+    SegWs(int64_t N, int G, int K, int M, gnn_dtype dtype, bool forward) {
+        const bool f32 = dtype == GNN_F32;
+        auto copy = [&](int64_t rows, int cols) -> size_t { return f32 ? up256(6 * (size_t)rows * up8(cols)) : cols % 8 ? up256(2 * (size_t)rows * up8(cols)) : 0; };
+        x = 256;
+        dy = x + copy(N, K);
+        w = dy + (forward ? 0 : copy(N, M));
+        part = w + copy((int64_t)G * K, M);
+        bytes = part;
+        bn = sg_block(M, f32 ? 128 : 256, 148);
+        tiles_n = (M + bn - 1) / bn;
+        tiles_m = (K + 127) / 128;
+        parts = dw_parts(N, (int64_t)tiles_n * tiles_m, f32);
+        if (!forward && parts > 1) bytes += (size_t)2 * parts * K * M * 4;
+    }
+};
+
+// the matrix as the products read it: itself, its padded copy, or its three planes at dst
+static const void* operand(const void* src, int64_t rows, int cols, gnn_dtype dtype, void* dst, cudaStream_t st) {
+    const int ld = up8(cols);
+    if (dtype == GNN_BF16 && cols == ld) return src;
+    const dim3 grid((unsigned)ceil_div(rows * (ld / 8), 256));
+    if (dtype == GNN_F32) launch_overlapped(split_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)src, rows, cols, (__nv_bfloat16*)dst, ld, (int)(cols % 4 == 0));
+    else launch_overlapped(split_rows_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, (const __nv_bfloat16*)src, rows, cols, (__nv_bfloat16*)dst, ld, 0);
+    return dst;
+}
+
+static const char* seg_shape_error(int32_t N, int G, int K, int M, gnn_dtype dtype) {
+    if (N < 0 || G < 0 || K <= 0 || M <= 0) return "bad shape";
+    if (dtype != GNN_F32 && dtype != GNN_BF16) return "bad dtype";
+    return nullptr;
+}
+static bool seg_size_ok(int32_t N, int G, int K, int M, gnn_dtype dtype) {
+    const int most = dtype == GNN_F32 ? 2048 : 8192;
+    return K <= most && M <= most && N < INT32_MAX - TC_ROWS && (int64_t)G * K <= ((int64_t)1 << 31) - 1 && G <= (1 << 24);
+}
+
+// Y = X * W (dx = false) or dX = dY * W^T (dx = true): in [N, cin], out [N, cout]
+static gnn_status seg_rows(const char* who, bool dx, const void* in, const void* w, const int64_t* seg_ptr, int32_t N, int G, int K, int M, gnn_dtype dtype,
+                           const float* bias, int relu, void* out, int* status, int reset, cudaStream_t st) {
+    const bool f32 = dtype == GNN_F32;
+    const int levels = f32 ? 3 : 1, cin = dx ? M : K, cout = dx ? K : M;
+    SegGemmParams P = {};
+    const int64_t row_tiles = (int64_t)N / TC_ROWS + G;
+    P.seg_ptr = seg_ptr; P.G = G; P.N = N;
+    P.bn = sg_block(cout, f32 ? 128 : 256, row_tiles);
+    P.tiles_n = (cout + P.bn - 1) / P.bn; P.tiles_m = 1;
+    P.units = row_tiles * P.tiles_n;
+    P.slices = (cin + 63) / 64;
+    P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
+    P.rows_out = TC_ROWS; P.cols_out = cout;
+    P.out = out; P.vec = (size_t)cout * elem_size(dtype) % 16 == 0;
+    P.bias = bias; P.relu = relu; P.status = status; P.reset = reset;
+    CUtensorMap mapA, mapB;
+    if (!make_map_planes(&mapA, in, false, levels, N, cin, up8(cin), P.a_rows) ||
+        !make_map_planes(&mapB, w, false, (int64_t)levels * G, K, M, up8(M), dx ? P.bn : 64))
+        GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
+    if (dx) return f32 ? sg_launch<SG_DX, 3, float>(who, LS_SLOT, mapA, mapB, P, st) : sg_launch<SG_DX, 1, __nv_bfloat16>(who, LS_SLOT + 1, mapA, mapB, P, st);
+    return f32 ? sg_launch<SG_Y, 3, float>(who, LS_SLOT + 2, mapA, mapB, P, st) : sg_launch<SG_Y, 1, __nv_bfloat16>(who, LS_SLOT + 3, mapA, mapB, P, st);
+}
+
+static gnn_status zero(const char* who, void* p, size_t bytes, cudaStream_t st) {
+    if (bytes && cudaMemsetAsync(p, 0, bytes, st) != cudaSuccess) GNN_FAIL(GNN_ERR_CUDA, "%s: memset failed (is it a device pointer?)", who);
+    return GNN_OK;
+}
+
+}  // namespace gnn
+
+using namespace gnn;
+
+extern "C" {
+
+size_t gnn_linear_segments_workspace(int32_t N, int G, int K, int M, gnn_dtype dtype, int backward) {
+    if (seg_shape_error(N, G, K, M, dtype)) return 0;
+    return SegWs(N, G, K, M, dtype, !backward).bytes;
+}
+
+gnn_status gnn_linear_segments(const void* X, const int64_t* seg_ptr, const void* W, int32_t N, int G, int K, int M, gnn_dtype dtype,
+                               const float* bias, int relu, void* Y, void* ws, size_t ws_bytes, gnn_stream stream) {
+    const char* who = "gnn_linear_segments";
+    const char* bad = seg_shape_error(N, G, K, M, dtype);
+    GNN_REQUIRE(!bad, GNN_ERR_INVALID_ARG, "%s: %s", who, bad);
+    GNN_REQUIRE(seg_size_ok(N, G, K, M, dtype), GNN_ERR_UNSUPPORTED, "%s: K and M up to 8192 (fp32: 2048), G K under 2^31", who);
+    GNN_REQUIRE(ws && ws_bytes >= 256, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace too small", who);
+    cudaStream_t st = as_stream(stream);
+    const gnn_status rs = zero(who, ws, N == 0 || G == 0 ? sizeof(int) : 0, st);
+    if (rs != GNN_OK || N == 0) return rs;
+    GNN_REQUIRE(Y, GNN_ERR_INVALID_ARG, "%s: null Y", who);
+    if (G == 0) return zero(who, Y, (size_t)N * M * elem_size(dtype), st);
+    GNN_REQUIRE(X && W && seg_ptr, GNN_ERR_INVALID_ARG, "%s: null argument", who);
+    GNN_REQUIRE(aligned16(X) && aligned16(W) && aligned16(Y) && aligned16(ws), GNN_ERR_INVALID_ARG, "%s: matrices and workspace must be 16-byte aligned", who);
+    const SegWs sw(N, G, K, M, dtype, true);
+    GNN_REQUIRE(ws_bytes >= sw.bytes, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed", who, sw.bytes);
+    GNN_REQUIRE(tensor_map_encoder_available(), GNN_ERR_CUDA, "%s: the driver has no tensor-map encoder", who);
+    char* const w8 = (char*)ws;
+    const void* Xp = operand(X, N, K, dtype, w8 + sw.x, st);
+    const void* Wp = operand(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
+    GNN_CHECK_LAUNCH(who);
+    return seg_rows(who, false, Xp, Wp, seg_ptr, N, G, K, M, dtype, bias, relu, Y, (int*)ws, 1, st);
+}
+
+gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, const void* W, const void* dY, int32_t N, int G, int K, int M,
+                                        gnn_dtype dtype, void* dX, void* dW, void* ws, size_t ws_bytes, gnn_stream stream) {
+    const char* who = "gnn_linear_segments_backward";
+    const char* bad = seg_shape_error(N, G, K, M, dtype);
+    GNN_REQUIRE(!bad, GNN_ERR_INVALID_ARG, "%s: %s", who, bad);
+    GNN_REQUIRE(seg_size_ok(N, G, K, M, dtype), GNN_ERR_UNSUPPORTED, "%s: K and M up to 8192 (fp32: 2048), G K under 2^31", who);
+    const SegWs sw(N, G, K, M, dtype, false);
+    GNN_REQUIRE(ws && ws_bytes >= sw.bytes, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed", who, sw.bytes);
+    cudaStream_t st = as_stream(stream);
+    const size_t s = (size_t)elem_size(dtype);
+    if (N == 0 || G == 0) {
+        gnn_status rc = zero(who, ws, sizeof(int), st);
+        if (rc == GNN_OK && dX) rc = zero(who, dX, (size_t)N * K * s, st);
+        if (rc == GNN_OK && dW) rc = zero(who, dW, (size_t)G * K * M * s, st);
+        return rc;
+    }
+    GNN_REQUIRE(dY && seg_ptr, GNN_ERR_INVALID_ARG, "%s: null argument", who);
+    GNN_REQUIRE(!dX || W, GNN_ERR_INVALID_ARG, "%s: dX needs W", who);
+    GNN_REQUIRE(!dW || X, GNN_ERR_INVALID_ARG, "%s: dW needs X", who);
+    GNN_REQUIRE(aligned16(dY) && (!dX || (aligned16(W) && aligned16(dX))) && (!dW || (aligned16(X) && aligned16(dW))) && aligned16(ws), GNN_ERR_INVALID_ARG,
+                "%s: matrices and workspace must be 16-byte aligned", who);
+    GNN_REQUIRE(tensor_map_encoder_available(), GNN_ERR_CUDA, "%s: the driver has no tensor-map encoder", who);
+    if (!dX && !dW) return zero(who, ws, sizeof(int), st);
+    char* const w8 = (char*)ws;
+    const bool f32 = dtype == GNN_F32;
+    const void* dYp = operand(dY, N, M, dtype, w8 + sw.dy, st);
+    int reset = 1;
+    if (dX) {
+        const void* Wp = operand(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
+        GNN_CHECK_LAUNCH(who);
+        const gnn_status rc = seg_rows(who, true, dYp, Wp, seg_ptr, N, G, K, M, dtype, nullptr, 0, dX, (int*)ws, reset, st);
+        if (rc != GNN_OK) return rc;
+        reset = 0;
+    }
+    if (dW) {
+        const void* Xp = operand(X, N, K, dtype, w8 + sw.x, st);
+        GNN_CHECK_LAUNCH(who);
+        SegGemmParams P = {};
+        P.seg_ptr = seg_ptr; P.G = G; P.N = N;
+        P.bn = sw.bn; P.tiles_n = sw.tiles_n; P.tiles_m = sw.tiles_m;
+        P.part_rows = ceil_div(N, sw.parts);
+        P.units = ceil_div(N, P.part_rows) * P.tiles_n * P.tiles_m;
+        P.rows_out = K; P.cols_out = M;
+        P.out = dW; P.vec = (size_t)M * s % 16 == 0;
+        P.part = (float*)(w8 + sw.part);
+        P.status = (int*)ws; P.reset = reset;
+        CUtensorMap mapA, mapB;
+        const int levels = f32 ? 3 : 1;
+        if (!make_map_planes(&mapA, Xp, false, levels, N, K, up8(K), 64) || !make_map_planes(&mapB, dYp, false, levels, N, M, up8(M), 64))
+            GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
+        const gnn_status rc = f32 ? sg_launch<SG_DW, 3, float>(who, LS_SLOT + 4, mapA, mapB, P, st) : sg_launch<SG_DW, 1, __nv_bfloat16>(who, LS_SLOT + 5, mapA, mapB, P, st);
+        if (rc != GNN_OK) return rc;
+        const int64_t size = (int64_t)K * M;
+        const dim3 grid((unsigned)ceil_div(size, 1024), (unsigned)(G < 65535 ? G : 65535));
+        if (f32) launch_overlapped(segment_sum_kernel<float>, grid, dim3(256), 0, st, seg_ptr, G, (int64_t)N, P.part_rows, (const float*)P.part, size, (float*)dW);
+        else launch_overlapped(segment_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, seg_ptr, G, (int64_t)N, P.part_rows, (const float*)P.part, size, (__nv_bfloat16*)dW);
+        GNN_CHECK_LAUNCH(who);
+    }
+    return GNN_OK;
+}
+
+}  // extern "C"

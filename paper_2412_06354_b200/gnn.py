@@ -119,6 +119,15 @@ SIGNATURES = {
     "gnn_propagate_linear": (_INT, [_CSR, _INT, _INT, _VP, _VP, _VP, _INT, _INT, _INT, _VP, _INT, _VP, _VP, _SZ, _VP]),
     "gnn_propagate_linear_backward": (_INT, [_CSR, _INT, _INT, _VP, _VP, _VP, _VP, _INT, _INT, _INT, _VP, _VP, _VP, _SZ, _VP]),
     "gnn_linear_backward": (_INT, [_VP, _VP, _VP, _I32, _INT, _INT, _INT, _VP, _VP, _VP, _SZ, _VP]),
+    "gnn_linear_segments_workspace": (_SZ, [_I32, _INT, _INT, _INT, _INT, _INT]),
+    "gnn_linear_segments": (_INT, [_VP, _VP, _VP, _I32, _INT, _INT, _INT, _INT, _VP, _INT, _VP, _VP, _SZ, _VP]),
+    "gnn_linear_segments_backward": (_INT, [_VP, _VP, _VP, _VP, _I32, _INT, _INT, _INT, _INT, _VP, _VP, _VP, _SZ, _VP]),
+    "gnn_quantize_rows": (_INT, [_VP, _I32, _INT, _INT, _VP, _VP, _VP]),
+    "gnn_linear_i8_workspace": (_SZ, [_I32, _INT, _INT]),
+    "gnn_linear_i8": (_INT, [_VP, _VP, _VP, _VP, _I32, _INT, _INT, _INT, _VP, _INT, _VP, _VP, _SZ, _VP]),
+    "gnn_log_probs_workspace": (_SZ, [_I32, _INT, _INT, _INT]),
+    "gnn_log_probs": (_INT, [_VP, _VP, _I32, _INT, _INT, _INT, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
+    "gnn_log_probs_backward": (_INT, [_VP, _VP, _VP, _VP, _VP, _VP, _I32, _INT, _INT, _VP, _VP]),
     "gnn_propagate_fused_host": (_INT, [_CSR, _INT, _INT, _VP, _VP, _INT, _INT, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
     "gnn_propagate_fused_backward_host": (_INT, [_CSR, _INT, _INT, _VP, _VP, _VP, _INT, _INT, _VP, _VP, _VP, _VP, _SZ, _VP]),
 }
@@ -434,3 +443,35 @@ def linear_backward(X, W, dY, want_dX=True, want_dW=True, ws=None, return_ws=Fal
 
 def axpby(alpha, a, beta, b, out=None):
     return _b.axpby(a, b, alpha, beta, out)
+
+
+# ------------------------------------------------------------------ typed, 8-bit and last layers
+def linear_segments(X, seg_ptr, W, bias=None, relu=False, ws=None, return_ws=False):
+    """act(X[i] W[g(i)] + bias[g(i)]) for rows sorted by segment: X [N,K], seg_ptr int64 [G+1], W [G,K,M], bias [G,M]."""
+    return _b.linear_segments(X, seg_ptr, W, bias, relu, ws, return_ws)
+
+
+def linear_segments_backward(X, seg_ptr, W, dY, want_dX=True, want_dW=True, ws=None, return_ws=False):
+    """-> (dX [N,K], dW [G,K,M]); X may be None without dW.  W gives the sizes and is needed either way."""
+    return _b.linear_segments_backward(X, seg_ptr, W, dY, want_dX, want_dW, ws, return_ws)
+
+
+def quantize_rows(X):
+    """-> (int8 rows, their fp32 scales); weights [K,M]: quantize_rows(W.t().contiguous()) once."""
+    return _b.quantize_rows(X)
+
+
+def linear_i8(xq, x_scale, wq, w_scale, bias=None, relu=False, dtype=torch.float32, ws=None, return_ws=False):
+    """act(x_scale[i] w_scale[m] <xq[i], wq[m]> + bias[m]) as dtype (float32 or bfloat16): xq [N,K], wq [M,K]."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported feature dtype {dtype}")
+    return _b.linear_i8(xq, x_scale, wq, w_scale, bias, relu, dtype == torch.bfloat16, ws, return_ws)
+
+
+def log_probs(Z, label=None, top=0, want_entropy=True, ws=None):
+    """-> (logp [N] or None, entropy [N] or None, lse [N], top_logp [N,top], top_idx [N,top])"""
+    return _b.log_probs(Z, label, top, want_entropy, ws)
+
+
+def log_probs_backward(Z, label, lse, dlogp=None, entropy=None, dentropy=None):
+    return _b.log_probs_backward(Z, label, lse, dlogp, entropy, dentropy)
