@@ -267,16 +267,16 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     P.bn = sg_block(M, 256, row_tiles);
     P.tiles_n = (M + P.bn - 1) / P.bn; P.tiles_m = 1;
     P.units = row_tiles * P.tiles_n;
-    P.slices = (K + 127) / 128;
+    P.slices = (K + 127) / 128; P.contraction = K;
     P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
     P.rows_out = TC_ROWS; P.cols_out = M;
     P.out = Y; P.vec = (size_t)M * elem_size(dtype) % 16 == 0;
     P.bias = bias; P.relu = relu; P.sx = x_scale; P.sw = w_scale;
     P.status = (int*)ws; P.reset = 1;
     CUtensorMap mapA, mapB;
-    if (!make_map_planes(&mapA, xp, true, 1, N, K, up16(K), P.a_rows) || !make_map_planes(&mapB, wp, true, 1, M, K, up16(K), P.bn))
+    if (!make_map_planes(&mapA, xp, 1, 1, N, K, up16(K), P.a_rows) || !make_map_planes(&mapB, wp, 1, 1, M, K, up16(K), P.bn))
         GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-    return dtype == GNN_F32 ? sg_launch<SG_I8, 1, float>(who, I8_SLOT, mapA, mapB, P, st) : sg_launch<SG_I8, 1, __nv_bfloat16>(who, I8_SLOT + 1, mapA, mapB, P, st);
+    return dtype == GNN_F32 ? sg_launch<SG_I8, float>(who, I8_SLOT, mapA, mapB, P, st) : sg_launch<SG_I8, __nv_bfloat16>(who, I8_SLOT + 1, mapA, mapB, P, st);
 }
 
 }  // extern "C"

@@ -1,18 +1,17 @@
 // Dense transform whose weight depends on the row's segment (the node types or relations of a heterogeneous graph):
 //   Y[i,:] = act(X[i,:] * W[g(i)] + bias[g(i)]),  dX[i,:] = dY[i,:] * W[g(i)]^T,  dW[g] = X_g^T * dY_g
-// Entry points, their workspaces and the small kernels around the products of segment_gemm.cuh: padded copies of bf16 matrices
-// whose rows do not start on 16 bytes, the three bf16 terms of fp32 matrices, the ordered sum of dW's partials.
+// Entry points, their workspaces and the small kernels around the products of segment_gemm.cuh: padded copies of matrices
+// whose rows do not start on 16 bytes, the three bf16 terms of fp32 weights, the ordered sum of dW's partials.
 #include "segment_gemm.cuh"
 
 namespace gnn {
 
 constexpr int LS_SLOT = 48;  // of allow_big_smem: six of them
 
-// Rows of fp32 as three planes of bf16 rows (x = x1 + x2 + x3 exactly), or bf16 rows on 16-byte starts (one plane): a thread
-// writes 8 elements of each plane.  Rows of dst are ld elements apart; what follows the last column is zero.
-template <typename T>
+// Rows of fp32 as three planes of bf16 rows (x = x1 + x2 + x3 exactly): a thread writes 8 elements of each plane.  Rows of dst
+// are ld elements apart; what follows the last column is zero.
 __global__ void __launch_bounds__(256)
-split_rows_kernel(const T* src, int64_t rows, int cols, __nv_bfloat16* __restrict__ dst, int ld, int vec) {
+split_rows_kernel(const float* src, int64_t rows, int cols, __nv_bfloat16* __restrict__ dst, int ld, int vec) {
     pdl_wait();
     const int chunks = ld / 8;
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
@@ -20,20 +19,16 @@ split_rows_kernel(const T* src, int64_t rows, int cols, __nv_bfloat16* __restric
     const int64_t r = i / chunks;
     const int c = (int)(i - r * chunks) * 8;
     float x[8];
-    const T* const p = src + r * cols + c;
+    const float* const p = src + r * cols + c;
     if (vec && c + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            Chunk<float>::unpack(ld_16(p), x);
-            Chunk<float>::unpack(ld_16(p + 4), x + 4);
-        } else {
-            Chunk<__nv_bfloat16>::unpack(ld_16(p), x);
-        }
+        Chunk<float>::unpack(ld_16(p), x);
+        Chunk<float>::unpack(ld_16(p + 4), x + 4);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = c + k < cols ? (float)p[k] : 0.f;
+        for (int k = 0; k < 8; ++k) x[k] = c + k < cols ? p[k] : 0.f;
     }
 #pragma unroll
-    for (int l = 0; l < (sizeof(T) == 4 ? 3 : 1); ++l) {
+    for (int l = 0; l < 3; ++l) {
         const uint4 v = Chunk<__nv_bfloat16>::pack(x);
         *reinterpret_cast<uint4*>(dst + (l * rows + r) * (int64_t)ld + c) = v;
         float t[8];
@@ -41,6 +36,21 @@ split_rows_kernel(const T* src, int64_t rows, int cols, __nv_bfloat16* __restric
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] -= t[k];  // exact: the rounded term shares the leading bits
     }
+}
+
+// rows on 16-byte starts, zeros behind the last column: a chunk of PER elements per thread
+template <typename E, int PER>
+__global__ void __launch_bounds__(256)
+widen_rows_kernel(const E* src, int64_t rows, int cols, E* __restrict__ dst, int chunks) {
+    pdl_wait();
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= rows * chunks) return;
+    const int64_t r = i / chunks;
+    const int c = (int)(i - r * chunks) * PER;
+    union { E e[PER]; uint4 v; } u;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) u.e[k] = c + k < cols ? src[r * cols + c + k] : E(0);
+    *reinterpret_cast<uint4*>(dst + (r * chunks) * PER + c) = u.v;
 }
 
 // dW of the segments that more than one part holds (their partials in ascending order) or none (zeros).  A block of 256
@@ -72,6 +82,8 @@ segment_sum_kernel(const int64_t* seg_ptr, int G, int64_t N, int64_t part_rows, 
 }
 
 static int up8(int x) { return (x + 7) & ~7; }
+// elements between rows that start on 16 bytes
+static int apart(int cols, gnn_dtype dtype) { return dtype == GNN_F32 ? (cols + 3) & ~3 : up8(cols); }
 
 // How the rows are cut for dW: parts x tiles blocks of work on 148 SMs.  Few parts mean few partials; as many as keep the SMs
 // busy: the smallest number whose last wave costs at most 5 % over the best of all numbers, parts of at least 256 rows.  And of
@@ -96,11 +108,11 @@ struct SegWs {
     int bn, tiles_n, tiles_m;
     SegWs(int64_t N, int G, int K, int M, gnn_dtype dtype, bool forward) {
         const bool f32 = dtype == GNN_F32;
-        auto copy = [&](int64_t rows, int cols) -> size_t { return f32 ? up256(6 * (size_t)rows * up8(cols)) : cols % 8 ? up256(2 * (size_t)rows * up8(cols)) : 0; };
+        auto copy = [&](int64_t rows, int cols) -> size_t { return apart(cols, dtype) != cols ? up256((size_t)elem_size(dtype) * rows * apart(cols, dtype)) : 0; };
         x = 256;
         dy = x + copy(N, K);
         w = dy + (forward ? 0 : copy(N, M));
-        part = w + copy((int64_t)G * K, M);
+        part = w + (f32 ? up256((size_t)6 * G * K * up8(M)) : copy((int64_t)G * K, M));
         bytes = part;
         bn = sg_block(M, f32 ? 128 : 256, 148);
         tiles_n = (M + bn - 1) / bn;
@@ -110,13 +122,20 @@ struct SegWs {
     }
 };
 
-// the matrix as the products read it: itself, its padded copy, or its three planes at dst
+// the matrix with rows on 16 bytes: itself or its copy at dst
 static const void* operand(const void* src, int64_t rows, int cols, gnn_dtype dtype, void* dst, cudaStream_t st) {
-    const int ld = up8(cols);
-    if (dtype == GNN_BF16 && cols == ld) return src;
-    const dim3 grid((unsigned)ceil_div(rows * (ld / 8), 256));
-    if (dtype == GNN_F32) launch_overlapped(split_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)src, rows, cols, (__nv_bfloat16*)dst, ld, (int)(cols % 4 == 0));
-    else launch_overlapped(split_rows_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, (const __nv_bfloat16*)src, rows, cols, (__nv_bfloat16*)dst, ld, 0);
+    const int ld = apart(cols, dtype);
+    if (cols == ld) return src;
+    const int chunks = ld * elem_size(dtype) / 16;
+    const dim3 grid((unsigned)ceil_div(rows * chunks, 256));
+    if (dtype == GNN_F32) launch_overlapped(widen_rows_kernel<float, 4>, grid, dim3(256), 0, st, (const float*)src, rows, cols, (float*)dst, chunks);
+    else launch_overlapped(widen_rows_kernel<uint16_t, 8>, grid, dim3(256), 0, st, (const uint16_t*)src, rows, cols, (uint16_t*)dst, chunks);
+    return dst;
+}
+// the weights: bf16 as above, fp32 as three planes
+static const void* weights(const void* W, int64_t rows, int M, gnn_dtype dtype, void* dst, cudaStream_t st) {
+    if (dtype == GNN_BF16) return operand(W, rows, M, dtype, dst, st);
+    launch_overlapped(split_rows_kernel, dim3((unsigned)ceil_div(rows * (up8(M) / 8), 256)), dim3(256), 0, st, (const float*)W, rows, M, (__nv_bfloat16*)dst, up8(M), (int)(M % 4 == 0));
     return dst;
 }
 
@@ -134,24 +153,24 @@ static bool seg_size_ok(int32_t N, int G, int K, int M, gnn_dtype dtype) {
 static gnn_status seg_rows(const char* who, bool dx, const void* in, const void* w, const int64_t* seg_ptr, int32_t N, int G, int K, int M, gnn_dtype dtype,
                            const float* bias, int relu, void* out, int* status, int reset, cudaStream_t st) {
     const bool f32 = dtype == GNN_F32;
-    const int levels = f32 ? 3 : 1, cin = dx ? M : K, cout = dx ? K : M;
+    const int cin = dx ? M : K, cout = dx ? K : M;
     SegGemmParams P = {};
     const int64_t row_tiles = (int64_t)N / TC_ROWS + G;
     P.seg_ptr = seg_ptr; P.G = G; P.N = N;
     P.bn = sg_block(cout, f32 ? 128 : 256, row_tiles);
     P.tiles_n = (cout + P.bn - 1) / P.bn; P.tiles_m = 1;
     P.units = row_tiles * P.tiles_n;
-    P.slices = (cin + 63) / 64;
+    P.slices = (cin + 63) / 64; P.contraction = cin;
     P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
     P.rows_out = TC_ROWS; P.cols_out = cout;
     P.out = out; P.vec = (size_t)cout * elem_size(dtype) % 16 == 0;
     P.bias = bias; P.relu = relu; P.status = status; P.reset = reset;
     CUtensorMap mapA, mapB;
-    if (!make_map_planes(&mapA, in, false, levels, N, cin, up8(cin), P.a_rows) ||
-        !make_map_planes(&mapB, w, false, (int64_t)levels * G, K, M, up8(M), dx ? P.bn : 64))
+    if (!make_map_planes(&mapA, in, f32 ? 2 : 0, 1, N, cin, apart(cin, dtype), P.a_rows) ||
+        !make_map_planes(&mapB, w, 0, (int64_t)(f32 ? 3 : 1) * G, K, M, up8(M), dx ? P.bn : 64))
         GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-    if (dx) return f32 ? sg_launch<SG_DX, 3, float>(who, LS_SLOT, mapA, mapB, P, st) : sg_launch<SG_DX, 1, __nv_bfloat16>(who, LS_SLOT + 1, mapA, mapB, P, st);
-    return f32 ? sg_launch<SG_Y, 3, float>(who, LS_SLOT + 2, mapA, mapB, P, st) : sg_launch<SG_Y, 1, __nv_bfloat16>(who, LS_SLOT + 3, mapA, mapB, P, st);
+    if (f32) return segment_gemm_f32(who, dx ? SG_DX : SG_Y, LS_SLOT + dx, mapA, mapB, P, st);
+    return dx ? sg_launch<SG_DX, __nv_bfloat16>(who, LS_SLOT + 2, mapA, mapB, P, st) : sg_launch<SG_Y, __nv_bfloat16>(who, LS_SLOT + 3, mapA, mapB, P, st);
 }
 
 static gnn_status zero(const char* who, void* p, size_t bytes, cudaStream_t st) {
@@ -189,7 +208,7 @@ gnn_status gnn_linear_segments(const void* X, const int64_t* seg_ptr, const void
     GNN_REQUIRE(tensor_map_encoder_available(), GNN_ERR_CUDA, "%s: the driver has no tensor-map encoder", who);
     char* const w8 = (char*)ws;
     const void* Xp = operand(X, N, K, dtype, w8 + sw.x, st);
-    const void* Wp = operand(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
+    const void* Wp = weights(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
     GNN_CHECK_LAUNCH(who);
     return seg_rows(who, false, Xp, Wp, seg_ptr, N, G, K, M, dtype, bias, relu, Y, (int*)ws, 1, st);
 }
@@ -222,7 +241,7 @@ gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, c
     const void* dYp = operand(dY, N, M, dtype, w8 + sw.dy, st);
     int reset = 1;
     if (dX) {
-        const void* Wp = operand(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
+        const void* Wp = weights(W, (int64_t)G * K, M, dtype, w8 + sw.w, st);
         GNN_CHECK_LAUNCH(who);
         const gnn_status rc = seg_rows(who, true, dYp, Wp, seg_ptr, N, G, K, M, dtype, nullptr, 0, dX, (int*)ws, reset, st);
         if (rc != GNN_OK) return rc;
@@ -241,10 +260,10 @@ gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, c
         P.part = (float*)(w8 + sw.part);
         P.status = (int*)ws; P.reset = reset;
         CUtensorMap mapA, mapB;
-        const int levels = f32 ? 3 : 1;
-        if (!make_map_planes(&mapA, Xp, false, levels, N, K, up8(K), 64) || !make_map_planes(&mapB, dYp, false, levels, N, M, up8(M), 64))
+        const int type = f32 ? 2 : 0, box_rows = f32 ? 32 : 64;
+        if (!make_map_planes(&mapA, Xp, type, 1, N, K, apart(K, dtype), box_rows) || !make_map_planes(&mapB, dYp, type, 1, N, M, apart(M, dtype), box_rows))
             GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-        const gnn_status rc = f32 ? sg_launch<SG_DW, 3, float>(who, LS_SLOT + 4, mapA, mapB, P, st) : sg_launch<SG_DW, 1, __nv_bfloat16>(who, LS_SLOT + 5, mapA, mapB, P, st);
+        const gnn_status rc = f32 ? segment_gemm_f32(who, SG_DW, LS_SLOT + 4, mapA, mapB, P, st) : sg_launch<SG_DW, __nv_bfloat16>(who, LS_SLOT + 5, mapA, mapB, P, st);
         if (rc != GNN_OK) return rc;
         const int64_t size = (int64_t)K * M;
         const dim3 grid((unsigned)ceil_div(size, 1024), (unsigned)(G < 65535 ? G : 65535));

@@ -9,11 +9,13 @@
 // with the smaller maximum, whose own maximum counts again: exp(m1 - m2) (s1 + 1).
 // The k best: keys of (score, lower index first) that are all different, sorted over the lanes of a warp; a chunk whose largest
 // score does not pass the worst of them is left alone.
-#include "common.cuh"
+#include "tc_common.cuh"
 
 namespace gnn {
 
-constexpr int LP_TOP = 32;  // classes listed at most: a lane each
+constexpr int LP_TOP = 32;            // classes listed at most: a lane each
+constexpr int LP_WARP_CLASSES = 1024;  // rows up to here by a warp
+constexpr int LP_SLOT = 56;           // of allow_big_smem: two of them
 
 __device__ __forceinline__ float lp_exp(float d) {  // exp of d <= 0: 2^(d log2 e); the error of the product reaches what is below e^-10 by 1e-6 of it
     float e;
@@ -65,6 +67,30 @@ __device__ __forceinline__ float lp_score(uint64_t key) {
     const uint32_t v = (uint32_t)(key >> 32);
     return v == 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float((v & 0x80000000u) ? v & 0x7FFFFFFFu : ~v);
 }
+
+// Sorting over the lanes of a warp, largest in lane 0 (bitonic: 15 exchanges; a merge of two sorted lists into the best 32: 6)
+template <typename V>
+__device__ __forceinline__ V lp_exchange(V v, int o, bool keep_larger) {
+    const V w = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return (v > w) == keep_larger ? v : w;
+}
+template <typename V>
+__device__ __forceinline__ V lp_sort(V v, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int o = size / 2; o > 0; o >>= 1) v = lp_exchange(v, o, ((lane & o) == 0) == ((lane & size) == 0 || size == 32));
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ V lp_merge(V a, V b, int lane) {  // both sorted
+    const V r = __shfl_sync(0xFFFFFFFFu, b, 31 - lane);
+    a = a > r ? a : r;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a = lp_exchange(a, o, (lane & o) == 0);
+    return a;
+}
+
 // the k best so far, lane j the j-th; last: the worst of them (0: not full)
 struct LpTop {
     uint64_t key, last;
@@ -85,6 +111,12 @@ struct LpTop {
         }
     }
 };
+// the best of n keys in shared memory, by one warp
+__device__ __forceinline__ uint64_t lp_best_of(const uint64_t* keys, int n, int lane) {
+    uint64_t best = 0;
+    for (int i = 0; i < n; i += 32) best = lp_merge(best, lp_sort(i + lane < n ? keys[i + lane] : 0, lane), lane);
+    return best;
+}
 
 struct LpParams {
     const void* z;
@@ -100,7 +132,7 @@ struct LpParams {
 
 // what a row answers, from its statistics (all lanes) and its best (a lane each)
 template <typename T>
-__device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const LpStats& st, const LpTop& best, int lane) {
+__device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const LpStats& st, uint64_t best, int lane) {
     const float nan = __uint_as_float(0x7FC00000u);
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
     const float tail = log1pf(st.s);
@@ -116,19 +148,124 @@ __device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const 
         }
     }
     if (lane < P.top) {
-        P.top_idx[row * P.top + lane] = (int32_t)lp_class(best.key);
-        P.top_logp[row * P.top + lane] = logp(lp_score(best.key));
+        P.top_idx[row * P.top + lane] = (int32_t)lp_class(best);
+        P.top_logp[row * P.top + lane] = logp(lp_score(best));
     }
 }
 
-// rows by W warps (1: eight rows a block; 8: a row, or a part of one, per block)
+// Few classes, many rows: a thread per row, its scores in registers (CM of them, those past the last one NaN, which no maximum
+// takes).  A block's rows are consecutive in memory: they arrive by whole chunks and are handed over through shared memory, rows
+// an odd number of words apart.  170,000 x 47, five best: by a warp per row 241 us.
+constexpr int LP_ROWS = 128;  // of a block
+
+template <typename T, int CM>
+__global__ void __launch_bounds__(LP_ROWS)
+log_probs_few_kernel(const LpParams P) {
+    pdl_wait();
+    constexpr int PER = Chunk<T>::N;
+    extern __shared__ float sh_z[];  // [LP_ROWS][C | 1]
+    const int C = P.C, stride = C | 1;
+    const int64_t r0 = (int64_t)blockIdx.x * LP_ROWS;
+    const int rows = (int)(P.N - r0 < LP_ROWS ? P.N - r0 : LP_ROWS);
+    const T* const z = (const T*)P.z + r0 * C;  // on 16 bytes: LP_ROWS rows are
+    const int elements = rows * C;
+    for (int e = (int)threadIdx.x * PER; e < elements; e += LP_ROWS * PER) {
+        float f[PER];
+        if (e + PER <= elements) Chunk<T>::unpack(ld_16(z + e), f);
+        else
+#pragma unroll
+            for (int k = 0; k < PER; ++k) f[k] = e + k < elements ? (float)z[e + k] : 0.f;
+        int r = (int)((unsigned)e / (unsigned)C), c = e - r * C;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (e + k < elements) sh_z[r * stride + c] = f[k];
+            if (++c == C) { c = 0; ++r; }
+        }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= rows) return;
+    const int64_t row = r0 + threadIdx.x;
+    const float* const mine = sh_z + threadIdx.x * stride;
+    const float nan = __uint_as_float(0x7FC00000u);
+    float v[CM];
+#pragma unroll
+    for (int c = 0; c < CM; ++c) v[c] = c < C ? mine[c] : nan;
+    auto largest = [&]() {
+        float m = v[0];
+#pragma unroll
+        for (int c = 1; c < CM; ++c) m = fmaxf(m, v[c]);
+        return m;
+    };
+    // the first class at m
+    auto where = [&](float m) {
+        int at = CM;
+#pragma unroll
+        for (int c = CM - 1; c >= 0; --c) at = v[c] == m ? c : at;
+        return at;
+    };
+    LpStats st;
+    st.clear();
+    st.m = largest();
+    const int lead = where(st.m);
+    const bool nothing = !(st.m > -INFINITY);  // -inf, or NaN throughout
+    if (nothing) st.m = -INFINITY;
+    const float base = nothing ? 0.f : st.m;
+#pragma unroll
+    for (int c = 0; c < CM; ++c) {
+        if (c >= C) break;
+        if (c != lead || nothing) st.add(v[c], base);
+    }
+    const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
+    const float tail = log1pf(st.s);
+    auto logp = [&](float x) { return bad ? nan : none || x == -INFINITY ? -INFINITY : (x - st.m) - tail; };
+    if (P.lse) P.lse[row] = bad ? nan : none ? -INFINITY : st.m + tail;
+    if (P.entropy) P.entropy[row] = bad ? nan : none ? 0.f : tail - st.t / (1.f + st.s);
+    if (P.logp) {
+        const int y = P.label[row];
+        P.logp[row] = y >= 0 && y < C ? logp(mine[y]) : 0.f;
+    }
+    float m = st.m;
+    int at = lead;
+    for (int j = 0; j < P.top; ++j) {
+        if (j > 0) {
+            m = largest();
+            at = where(m);
+        }
+        if (at >= C) {  // numbers are used up: what is not one, in order
+            int skip = j;  // classes listed so far that are not numbers: all but the numbers before
+            for (int c = 0; c < C; ++c) skip -= mine[c] == mine[c];
+            if (skip < 0) skip = 0;
+            for (int c = 0; c < C; ++c)
+                if (mine[c] != mine[c] && skip-- == 0) at = c;
+            m = nan;
+        }
+        P.top_idx[row * P.top + j] = at;
+        P.top_logp[row * P.top + j] = logp(m);
+#pragma unroll
+        for (int c = 0; c < CM; ++c) v[c] = c == at ? nan : v[c];
+    }
+}
+
+// Rows by W warps (1: eight rows a block; 8: a row, or a part of one, per block), in one pass over the scores.
+// The best classes: every thread keeps the largest score of each of its chunks (shared memory).  The k-th largest of the
+// threads' own largest scores is a floor of the k-th best class; only chunks that reach it are looked at again (in L1 or L2),
+// about k of thousands, and what reaches it in them is sorted.  Where that gives fewer than k classes or more than LP_CAND (many
+// equal scores, rows masked nearly throughout, scores that are not numbers) the classes are offered to a sorted list one by
+// one.  (Offered one by one always, 256 x 170,000 bf16, ten best: 175 us.)
+constexpr int LP_CAND = 256;
+constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory
+
 template <typename T, int W>
 __global__ void __launch_bounds__(256)
 log_probs_kernel(const LpParams P) {
     pdl_wait();
     constexpr int PER = Chunk<T>::N;
+    extern __shared__ float sh_max[];  // [chunks of a thread][256]
     __shared__ LpStats sh_stats[8];
-    __shared__ uint64_t sh_keys[8][LP_TOP];
+    __shared__ uint64_t sh_cand[W == 1 ? 8 : 1][LP_CAND];
+    __shared__ uint64_t sh_keys[W == 1 ? 1 : 8][LP_TOP];
+    __shared__ float sh_sorted[W == 1 ? 1 : 8][32], sh_floor;
+    __shared__ int sh_count[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + warp : (int64_t)blockIdx.x / P.parts;
     const int part = W == 1 ? 0 : (int)(blockIdx.x % P.parts);
@@ -142,45 +279,48 @@ log_probs_kernel(const LpParams P) {
         c1 = n1 < c1 ? n1 : c1;
         c0 = n0;
     }
-    LpStats st;
-    LpTop best;
-    st.clear();
-    best.clear();
-    constexpr int U = 4;  // chunks in flight per lane
     const int me = W == 1 ? lane : threadIdx.x;
     constexpr int STEP = W * 32;
+    // chunk i of the matrix; elements outside the row: -inf, and not `in`
+    auto load = [&](int64_t i) {
+        if ((i + 1) * PER <= all) return ld_16(z + i * PER);
+        union { T e[PER]; uint4 q; } x;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) x.e[k] = i * PER + k < all ? z[i * PER + k] : T(0.f);
+        return x.q;
+    };
+    auto inside = [&](int64_t i, int k) { return i * PER + k >= e0 && i * PER + k < e1; };
+    LpStats st;
+    st.clear();
+    float mine = -INFINITY;
+    const bool list = P.top > 0;
+    constexpr int U = 4;  // chunks in flight per lane
+    int n = 0;
     for (int64_t c = c0; c < c1; c += U * STEP) {  // the same for all lanes
         uint4 v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = c + u * STEP + me;
-            if (i < c1) {
-                if ((i + 1) * PER <= all) v[u] = ld_16(z + i * PER);
-                else {
-                    union { T e[PER]; uint4 q; } x;
-#pragma unroll
-                    for (int k = 0; k < PER; ++k) x.e[k] = i * PER + k < all ? z[i * PER + k] : T(0.f);
-                    v[u] = x.q;
-                }
-            }
+            if (i < c1) v[u] = load(i);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (c + u * STEP >= c1) break;  // uniform
             const int64_t i = c + u * STEP + me;
+            if (i >= c1) break;
             float f[PER];
             Chunk<T>::unpack(v[u], f);
-            const bool on = i < c1;
-            const bool edge = !on || i * PER < e0 || (i + 1) * PER > e1;
-            bool in[PER];
+            if (i * PER < e0 || (i + 1) * PER > e1) {
 #pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                in[k] = !edge || (on && i * PER + k >= e0 && i * PER + k < e1);
-                if (!in[k]) f[k] = -INFINITY;
+                for (int k = 0; k < PER; ++k)
+                    if (!inside(i, k)) f[k] = -INFINITY;
             }
             float cm = f[0];
 #pragma unroll
             for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
+            if (list) {
+                sh_max[n * 256 + threadIdx.x] = cm;
+                ++n;
+            }
             if (cm > st.m) {
                 st.raise(cm);
                 bool taken = false;
@@ -195,16 +335,9 @@ log_probs_kernel(const LpParams P) {
 #pragma unroll
                 for (int k = 0; k < PER; ++k) st.add(f[k], base);
             }
-            if (P.top > 0) {
-                // a class in an earlier chunk wins a tie: only a larger score passes, once the list is full
-                const bool passes = (best.last >> 32) <= 1u ? on : cm > lp_score(best.last);
-                if (__any_sync(0xFFFFFFFFu, passes)) {
-#pragma unroll
-                    for (int k = 0; k < PER; ++k) best.offer(passes && in[k] ? lp_key(f[k], (uint32_t)(i * PER + k - e0)) : 0, P.top, lane);
-                }
-            }
         }
     }
+    mine = st.m;  // its own largest score
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         LpStats q;
@@ -214,45 +347,138 @@ log_probs_kernel(const LpParams P) {
         // both sides of a pair join in the same order
         if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
     }
+    uint64_t best = 0;
+    if (list) {
+        float floor = lp_sort(mine, lane);
+        const int g = W == 1 ? warp : 0;
+        if (lane == 0) sh_count[warp] = 0;
+        if constexpr (W == 1) {
+            floor = __shfl_sync(0xFFFFFFFFu, floor, P.top - 1);
+            __syncwarp();
+        } else {
+            sh_sorted[warp][lane] = floor;
+            __syncthreads();
+            if (warp == 0) {
+                for (int w = 1; w < W; ++w) floor = lp_merge(floor, sh_sorted[w][lane], lane);
+                if (lane == P.top - 1) sh_floor = floor;
+            }
+            __syncthreads();
+            floor = sh_floor;
+        }
+        for (int k = 0; k < n; ++k) {
+            if (!(sh_max[k * 256 + threadIdx.x] >= floor)) continue;
+            const int64_t i = c0 + (int64_t)k * STEP + me;
+            float f[PER];
+            Chunk<T>::unpack(load(i), f);
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (f[e] >= floor && inside(i, e)) {
+                    const int at = atomicAdd(&sh_count[g], 1);
+                    if (at < LP_CAND) sh_cand[g][at] = lp_key(f[e], (uint32_t)(i * PER + e - e0));
+                }
+        }
+        if constexpr (W == 1) __syncwarp(); else __syncthreads();
+        const int count = sh_count[g];
+        if (count >= P.top && count <= LP_CAND) {
+            if (W == 1 || warp == 0) best = lp_best_of(sh_cand[g], count, lane);
+        } else {
+            LpTop one;
+            one.clear();
+            for (int64_t c = c0; c < c1; c += STEP) {
+                const int64_t i = c + me;
+                float f[PER];
+                if (i < c1) Chunk<T>::unpack(load(i), f);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) one.offer(i < c1 && inside(i, e) ? lp_key(f[e], (uint32_t)(i * PER + e - e0)) : 0, P.top, lane);
+            }
+            best = one.key;
+            if constexpr (W > 1) {
+                sh_keys[warp][lane] = best;
+                __syncthreads();
+                if (warp == 0)
+                    for (int w = 1; w < W; ++w) best = lp_merge(best, sh_keys[w][lane], lane);
+            }
+        }
+    }
     if constexpr (W > 1) {
         if (lane == 0) sh_stats[warp] = st;
-        sh_keys[warp][lane] = best.key;
         __syncthreads();
         if (warp != 0) return;
-        for (int w = 1; w < W; ++w) {
-            st.join(sh_stats[w]);
-            if (P.top > 0) best.offer(lane < P.top ? sh_keys[w][lane] : 0, P.top, lane);
-        }
+        for (int w = 1; w < W; ++w) st.join(sh_stats[w]);
         if (P.parts > 1) {
             const int64_t at = row * P.parts + part;
             if (lane == 0) { P.stats[at * 4] = st.m; P.stats[at * 4 + 1] = st.s; P.stats[at * 4 + 2] = st.t; }
-            if (lane < P.top) P.keys[at * P.top + lane] = best.key;
+            if (lane < P.top) P.keys[at * P.top + lane] = best;
             return;
         }
     }
     lp_finish<T>(P, row, st, best, lane);
 }
 
-// the parts of a row joined in ascending order: a warp per row
+// The parts of a row joined: a block per row.  Only parts whose best class is among the k best such can hold one of the k best.
 template <typename T>
 __global__ void __launch_bounds__(256)
 log_probs_join_kernel(const LpParams P) {
     pdl_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= P.N) return;
+    __shared__ LpStats sh_stats[8];
+    __shared__ uint64_t sh_keys[8][32], sh_cand[LP_TOP * LP_TOP], sh_floor;
+    __shared__ int sh_count;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = blockIdx.x, first = row * P.parts;
     LpStats st;
-    LpTop best;
     st.clear();
-    best.clear();
-    for (int p = 0; p < P.parts; ++p) {
-        const int64_t at = row * P.parts + p;
-        LpStats q;
-        q.m = P.stats[at * 4]; q.s = P.stats[at * 4 + 1]; q.t = P.stats[at * 4 + 2];
-        st.join(q);
-        if (P.top > 0) best.offer(lane < P.top ? P.keys[at * P.top + lane] : 0, P.top, lane);
+    uint64_t top = 0;  // of this warp's parts, their best classes
+    for (int p0 = warp * 32; p0 < P.parts; p0 += 256) {
+        const int p = p0 + lane;
+        uint64_t k = 0;
+        if (p < P.parts) {
+            const float4 v = *reinterpret_cast<const float4*>(P.stats + (first + p) * 4);
+            LpStats q;
+            q.m = v.x; q.s = v.y; q.t = v.z;
+            st.join(q);
+            if (P.top > 0) k = P.keys[(first + p) * P.top];
+        }
+        if (P.top > 0) top = lp_merge(top, lp_sort(k, lane), lane);
     }
-    lp_finish<T>(P, row, st, best, lane);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        LpStats q;
+        q.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, o);
+        q.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, o);
+        q.t = __shfl_xor_sync(0xFFFFFFFFu, st.t, o);
+        if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
+    }
+    if (lane == 0) sh_stats[warp] = st;
+    sh_keys[warp][lane] = top;
+    if (threadIdx.x == 0) sh_count = 0;
+    __syncthreads();
+    if (P.top > 0) {
+        if (warp == 0) {
+            for (int w = 1; w < 8; ++w) top = lp_merge(top, sh_keys[w][lane], lane);
+            if (lane == P.top - 1) sh_floor = top;  // 0 where there are fewer parts than that: all of them count
+        }
+        __syncthreads();
+        const uint64_t floor = sh_floor;
+        // keys differ, so that at most `top` parts pass, with `top` keys each: they fit
+        const int parts = P.parts;
+        if (floor > 0) {
+            for (int p = threadIdx.x; p < parts; p += 256)
+                for (int j = 0; j < P.top; ++j) {
+                    const uint64_t k = P.keys[(first + p) * P.top + j];
+                    if (k < floor) break;
+                    sh_cand[atomicAdd(&sh_count, 1)] = k;
+                }
+        } else {
+            for (int64_t i = threadIdx.x; i < (int64_t)parts * P.top; i += 256) {
+                const uint64_t k = P.keys[first * P.top + i];
+                if (k) sh_cand[atomicAdd(&sh_count, 1)] = k;  // fewer than `top` parts have any
+            }
+        }
+        __syncthreads();
+    }
+    if (warp != 0) return;
+    for (int w = 1; w < 8; ++w) st.join(sh_stats[w]);
+    lp_finish<T>(P, row, st, P.top > 0 ? lp_best_of(sh_cand, sh_count, lane) : 0, lane);
 }
 
 struct LpGradParams {
@@ -264,8 +490,75 @@ struct LpGradParams {
     void* dz;
 };
 
-// a chunk of 16 bytes per thread and step, whatever rows its elements lie in
+// what a row's gradient needs; none: nothing to choose from, so that nothing depends on the scores
+struct LpRow {
+    float lse, H, g, h;
+    int y;
+    bool none;
+    __device__ __forceinline__ void read(const LpGradParams& P, int64_t row) {
+        lse = P.lse[row];
+        none = lse < -1e30f;
+        y = P.label ? P.label[row] : -1;
+        g = P.dlogp && y >= 0 && y < P.C && !none ? P.dlogp[row] : 0.f;
+        h = P.dentropy ? P.dentropy[row] : 0.f;
+        H = P.dentropy ? P.entropy[row] : 0.f;
+    }
+    // without the label's own share.  A class at -inf: p = 0 times a finite value
+    __device__ __forceinline__ float operator()(float z) const {
+        const float lp = z - lse;
+        return none ? 0.f : -lp_exp(lp) * fmaf(h, fmaxf(lp, -1e30f) + H, g);
+    }
+};
+
+// Long rows: a block takes LG_CHUNKS chunks of 16 bytes of one row.  Chunks that two rows share are written by both, element by
+// element.  2048 x 50,000 bf16 by the kernel below, which divides to find a chunk's row: 173 us.
+constexpr int LG_PER = 4, LG_CHUNKS = 256 * LG_PER;
+
 template <typename T>
+__global__ void __launch_bounds__(256)
+log_probs_backward_rows_kernel(const LpGradParams P, int parts) {
+    pdl_wait();
+    constexpr int PER = Chunk<T>::N;
+    const int64_t row = blockIdx.x / parts, all = P.N * P.C;
+    const int64_t e0 = row * P.C, e1 = e0 + P.C, c1 = (e1 + PER - 1) / PER;
+    const int64_t c0 = e0 / PER + (int64_t)(blockIdx.x % parts) * LG_CHUNKS + threadIdx.x;
+    const T* const z = (const T*)P.z;
+    T* const dz = (T*)P.dz;
+    LpRow R;
+    R.read(P, row);
+    const int64_t hit = R.y >= 0 && R.y < P.C ? e0 + R.y : -1;
+    uint4 v[LG_PER];
+#pragma unroll
+    for (int u = 0; u < LG_PER; ++u) {
+        const int64_t i = c0 + u * 256;
+        if (i < c1 && (i + 1) * PER <= all) v[u] = ld_16(z + i * PER);
+    }
+#pragma unroll
+    for (int u = 0; u < LG_PER; ++u) {
+        const int64_t i = c0 + u * 256;
+        if (i >= c1) break;
+        if (i * PER >= e0 && (i + 1) * PER <= e1) {
+            float f[PER];
+            Chunk<T>::unpack(v[u], f);
+#pragma unroll
+            for (int k = 0; k < PER; ++k) f[k] = R(f[k]);
+            if (hit >= i * PER && hit < (i + 1) * PER) {
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (hit == i * PER + k) f[k] += R.g;
+            }
+            *reinterpret_cast<uint4*>(dz + i * PER) = Chunk<T>::pack(f);
+        } else {
+            for (int k = 0; k < PER; ++k) {
+                const int64_t e = i * PER + k;
+                if (e >= e0 && e < e1) dz[e] = T(R((float)z[e]) + (e == hit ? R.g : 0.f));
+            }
+        }
+    }
+}
+
+// short rows: a chunk of 16 bytes per thread and step, whatever rows its elements lie in
+template <typename T, typename I>
 __global__ void __launch_bounds__(256)
 log_probs_backward_kernel(const LpGradParams P) {
     pdl_wait();
@@ -278,33 +571,17 @@ log_probs_backward_kernel(const LpGradParams P) {
         else
 #pragma unroll
             for (int k = 0; k < PER; ++k) f[k] = i * PER + k < all ? (float)((const T*)P.z)[i * PER + k] : 0.f;
-        int64_t row = i * PER / P.C;
+        int64_t row = (I)(i * PER) / (I)P.C;
         int c = (int)(i * PER - row * P.C);
-        int y = -1;
-        float lse = 0.f, H = 0.f, g = 0.f, h = 0.f;
-        bool fresh = true, none = false;
+        LpRow R;
+        R.read(P, row);
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            if (row < P.N) {
-                if (fresh) {
-                    lse = P.lse[row];
-                    y = P.label ? P.label[row] : -1;
-                    g = P.dlogp && y >= 0 && y < P.C ? P.dlogp[row] : 0.f;
-                    h = P.dentropy ? P.dentropy[row] : 0.f;
-                    H = P.dentropy ? P.entropy[row] : 0.f;
-                    none = lse < -1e30f;
-                    if (none) g = 0.f;  // nothing to choose from: nothing depends on the scores
-                    fresh = false;
-                }
-                // a class at -inf has no share, also in a row of nothing else (lse = -inf)
-                float d = 0.f;
-                if (f[k] != -INFINITY && !none) {
-                    const float lp = f[k] - lse;
-                    d = -__expf(lp) * fmaf(h, lp + H, g);
-                }
-                f[k] = c == y ? d + g : d;
+            f[k] = R(f[k]) + (c == R.y ? R.g : 0.f);
+            if (++c == P.C) {
+                c = 0;
+                if (++row < P.N && k + 1 < PER) R.read(P, row);
             }
-            if (++c == P.C) { c = 0; ++row; fresh = true; }
         }
         if (whole) *reinterpret_cast<uint4*>((T*)P.dz + i * PER) = Chunk<T>::pack(f);
         else
@@ -314,19 +591,24 @@ log_probs_backward_kernel(const LpGradParams P) {
     }
 }
 
-// blocks per row: one, or as many as fill the SMs while each has 16 KB of the row at least
-static int lp_parts(int64_t N, int64_t C, int s) {
-    if (C * s < 32 * 1024 || N >= 148 * 4) return 1;
-    int64_t p = (148 * 8 + N - 1) / N;
-    const int64_t most = C * s / (16 * 1024);
-    return (int)(p < most ? p : most > 1 ? most : 1);
+// Blocks per row: as many as give the SMs eight blocks each while every block has 8 KB of the row at least; and enough that a
+// thread has LP_CHUNKS chunks at most.
+static int64_t lp_parts(int64_t N, int64_t C, int s) {
+    const int64_t bytes = C * s, least = ceil_div(bytes + 16, (int64_t)LP_CHUNKS * 256 * 16 - 16);
+    int64_t p = N < 148 * 4 ? (148 * 8) / N : 1;
+    const int64_t most = bytes / (8 * 1024);
+    p = p < most ? p : most;
+    return p > least ? p : least;
 }
 
+// a thread per row: few classes, and rows enough to fill the SMs with threads
+static bool lp_few(int64_t N, int C, int top) { return C <= 64 && N >= 4096; }
+
 struct LpWs {
-    int parts;
+    int64_t parts;
     size_t keys, bytes;
     LpWs(int64_t N, int C, int top, gnn_dtype dtype) {
-        parts = N > 0 ? lp_parts(N, C, elem_size(dtype)) : 1;
+        parts = N > 0 && C > LP_WARP_CLASSES ? lp_parts(N, C, elem_size(dtype)) : 1;
         keys = parts > 1 ? up256((size_t)N * parts * 16) : 0;
         bytes = keys + (parts > 1 ? up256((size_t)N * parts * top * 8) : 0);
     }
@@ -360,19 +642,33 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
     LpParams P;
     P.z = Z; P.label = label; P.N = N; P.C = C; P.top = top;
     P.logp = logp; P.entropy = entropy; P.lse = lse; P.top_logp = top_logp; P.top_idx = top_idx;
-    P.parts = lw.parts; P.stats = (float*)ws; P.keys = (uint64_t*)((char*)ws + lw.keys);
+    P.parts = (int)lw.parts; P.stats = (float*)ws; P.keys = (uint64_t*)((char*)ws + lw.keys);
     const bool f32 = dtype == GNN_F32;
-    if (C <= 1024) {
+    const int64_t chunks = (int64_t)C / (f32 ? 4 : 8) + 2;  // of a row, both ends cut
+    if (lp_few(N, C, top)) {
+        const dim3 grid((unsigned)ceil_div(N, LP_ROWS));
+        const size_t smem = (size_t)LP_ROWS * (C | 1) * 4;
+        auto run = [&](auto kernel) { launch_overlapped(kernel, grid, dim3(LP_ROWS), smem, st, P); };
+        if (f32) C <= 8 ? run(log_probs_few_kernel<float, 8>) : C <= 16 ? run(log_probs_few_kernel<float, 16>) : C <= 32 ? run(log_probs_few_kernel<float, 32>)
+               : C <= 48 ? run(log_probs_few_kernel<float, 48>) : run(log_probs_few_kernel<float, 64>);
+        else C <= 8 ? run(log_probs_few_kernel<__nv_bfloat16, 8>) : C <= 16 ? run(log_probs_few_kernel<__nv_bfloat16, 16>) : C <= 32 ? run(log_probs_few_kernel<__nv_bfloat16, 32>)
+           : C <= 48 ? run(log_probs_few_kernel<__nv_bfloat16, 48>) : run(log_probs_few_kernel<__nv_bfloat16, 64>);
+    } else if (C <= LP_WARP_CLASSES) {
         const dim3 grid((unsigned)ceil_div(N, 8));
-        if (f32) launch_overlapped(log_probs_kernel<float, 1>, grid, dim3(256), 0, st, P);
-        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, st, P);
+        const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32) * 1024 : 0;
+        if (f32) launch_overlapped(log_probs_kernel<float, 1>, grid, dim3(256), smem, st, P);
+        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 1>, grid, dim3(256), smem, st, P);
     } else {
         const int64_t blocks = (int64_t)N * lw.parts;
         GNN_REQUIRE(blocks <= INT32_MAX, GNN_ERR_UNSUPPORTED, "%s: too many rows", who);
-        if (f32) launch_overlapped(log_probs_kernel<float, 8>, dim3((unsigned)blocks), dim3(256), 0, st, P);
-        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 8>, dim3((unsigned)blocks), dim3(256), 0, st, P);
+        const size_t smem = top > 0 ? (size_t)ceil_div(ceil_div(chunks, lw.parts), 256) * 1024 : 0;
+        const gnn_status rc = f32 ? allow_big_smem(who, (const void*)log_probs_kernel<float, 8>, LP_SLOT, LP_CHUNKS * 1024)
+                                  : allow_big_smem(who, (const void*)log_probs_kernel<__nv_bfloat16, 8>, LP_SLOT + 1, LP_CHUNKS * 1024);
+        if (rc != GNN_OK) return rc;
+        if (f32) launch_overlapped(log_probs_kernel<float, 8>, dim3((unsigned)blocks), dim3(256), smem, st, P);
+        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 8>, dim3((unsigned)blocks), dim3(256), smem, st, P);
         if (lw.parts > 1) {
-            const dim3 grid((unsigned)ceil_div(N, 8));
+            const dim3 grid((unsigned)N);
             if (f32) launch_overlapped(log_probs_join_kernel<float>, grid, dim3(256), 0, st, P);
             else launch_overlapped(log_probs_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, P);
         }
@@ -394,10 +690,18 @@ gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const flo
     cudaStream_t st = as_stream(stream);
     LpGradParams P;
     P.z = Z; P.label = label; P.N = N; P.C = C; P.lse = lse; P.entropy = entropy; P.dlogp = dlogp; P.dentropy = dentropy; P.dz = dZ;
-    const int64_t chunks = ceil_div((int64_t)N * C, dtype == GNN_F32 ? 4 : 8);
-    const dim3 grid((unsigned)grid_for(chunks, 256));
-    if (dtype == GNN_F32) launch_overlapped(log_probs_backward_kernel<float>, grid, dim3(256), 0, st, P);
-    else launch_overlapped(log_probs_backward_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, P);
+    const int per = dtype == GNN_F32 ? 4 : 8;
+    const int64_t parts = ceil_div((int64_t)C / per + 2, LG_CHUNKS), blocks = parts * N;
+    if (C >= 2048 && blocks <= INT32_MAX) {
+        if (dtype == GNN_F32) launch_overlapped(log_probs_backward_rows_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
+        else launch_overlapped(log_probs_backward_rows_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
+    } else {
+        const dim3 grid((unsigned)grid_for(ceil_div((int64_t)N * C, per), 256));
+        auto run = [&](auto kernel) { launch_overlapped(kernel, grid, dim3(256), 0, st, P); };
+        const bool narrow = (int64_t)N * C + 8 <= UINT32_MAX;  // the division that finds a chunk's row
+        if (dtype == GNN_F32) narrow ? run(log_probs_backward_kernel<float, uint32_t>) : run(log_probs_backward_kernel<float, int64_t>);
+        else narrow ? run(log_probs_backward_kernel<__nv_bfloat16, uint32_t>) : run(log_probs_backward_kernel<__nv_bfloat16, int64_t>);
+    }
     GNN_CHECK_LAUNCH(who);
     return GNN_OK;
 }

@@ -26,11 +26,9 @@
 //              not do: they may hold infinities)
 //   warps 2-9  epilogue: accumulator -> registers -> swizzled staging -> whole rows to global memory, rows and columns that do
 //              not exist left out
-// LEVELS = 3: fp32 values arrive as three bf16 terms (x = x1 + x2 + x3 exactly, written by split_rows_kernel); the six products
-// of levels with i + j <= 4 are added, the five small ones in an accumulator of their own: tensor-core sums cut off what lies
-// under the last bit of a 24-bit sum, which costs least where the large term meets a sum of few terms.
+// fp32 (segment_gemm_f32_kernel): the same pieces of work, every value as three bf16 terms.
 //
-// Every wait has an iteration limit; see linear_tma.cu.
+// Every wait has an iteration limit, as in linear_tma.cu.
 #pragma once
 #include <cuda.h>
 
@@ -45,7 +43,7 @@ enum { SG_Y = 0, SG_DX = 1, SG_DW = 2, SG_I8 = 3 };
 constexpr int SG_EPI_WARPS = 8;
 constexpr int SG_THREADS = 32 * (2 + SG_EPI_WARPS);
 constexpr int SG_MAX_STAGES = 8;
-constexpr size_t SG_SMEM_MAX = 225 * 1024;
+constexpr size_t SG_SMEM_MAX = 224 * 1024;      // dynamic; with the static part on its 1024-byte boundary: the 227 KB of a block
 constexpr uint32_t SG_A_BYTES = 128 * 128;      // 128 rows of 128 bytes (SG_DW: two boxes of 64 features x 64 rows)
 constexpr uint32_t SG_STAGING = 32 * 128;       // per epilogue warp
 constexpr uint32_t SG_SW128 = 2;
@@ -55,9 +53,9 @@ struct SegGemmParams {
     int G;
     int64_t N;
     int64_t units;           // tiles (SG_DW: parts x blocks of the result)
-    int slices;              // of the contraction (not SG_DW)
+    int slices, contraction; // (not SG_DW) slices of the contraction, its elements
     int tiles_n, tiles_m;    // blocks of output columns; of features (SG_DW)
-    int bn;                  // output columns of a tile: a multiple of 64, at most 256 / LEVELS
+    int bn;                  // output columns of a tile: a multiple of 64, at most 256, fp32 128
     int stages, tmem_cols;
     int a_rows;              // rows of a box of A (not SG_DW): 128, fewer where there are fewer in all
     int64_t part_rows;       // SG_DW: rows of a part
@@ -130,9 +128,28 @@ __device__ __forceinline__ uint64_t policy_normal() {
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-// levels of A and B of product q, small terms first: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-__device__ __forceinline__ constexpr uint32_t sg_pair_a(int q) { return q == 0 ? 2u : q == 2 || q == 3 ? 1u : 0u; }
-__device__ __forceinline__ constexpr uint32_t sg_pair_b(int q) { return q == 1 ? 2u : q == 2 || q == 4 ? 1u : 0u; }
+// Every role of a CTA walks the same pieces of work: body(rows of one segment, block of features, block of columns, part) until
+// it says stop.
+template <int MODE, class Body>
+__device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
+    for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
+        const int n = (int)(u % P.tiles_n);
+        if constexpr (MODE != SG_DW) {
+            const SegRows t = seg_tile(P, u / P.tiles_n);
+            if (t.hi > t.lo && !body(t, 0, n, (int64_t)0)) return;
+        } else {
+            const int64_t v = u / P.tiles_n, part = v / P.tiles_m;
+            const int64_t r0 = part * P.part_rows, r1 = r0 + P.part_rows < P.N ? r0 + P.part_rows : P.N;
+            int g = last_segment(P.G, [&](int q) { return seg_at(P, q) <= r0; });
+            for (g = g < 0 ? 0 : g; g < P.G; ++g) {
+                const int64_t a = seg_at(P, g), b = seg_at(P, g + 1);
+                if (a >= r1) break;
+                const SegRows t = {a > r0 ? a : r0, b < r1 ? b : r1, g};
+                if (t.hi > t.lo && !body(t, (int)(v % P.tiles_m), n, part)) return;
+            }
+        }
+    }
+}
 
 __device__ __forceinline__ void sg_store(float* p, uint32_t bits) { *reinterpret_cast<uint32_t*>(p) = bits; }
 __device__ __forceinline__ void sg_store(__nv_bfloat16* p, uint32_t bits) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)bits; }
@@ -170,23 +187,37 @@ __device__ __forceinline__ void sg_rows_out(uint32_t stg, T* out, int64_t ld, in
         }
 }
 
+// rows of no segment: zeros, by the epilogue warps (threads 64 .. 319 of each block)
+template <typename T>
+__device__ __forceinline__ void sg_zero_outside(const SegGemmParams& P, T* out) {
+    const int64_t p0 = seg_at(P, 0) * P.cols_out, p1 = seg_at(P, P.G) * P.cols_out, end = P.N * P.cols_out;
+    const int64_t me = (int64_t)blockIdx.x * (32 * SG_EPI_WARPS) + ((int)threadIdx.x - 64), all = (int64_t)gridDim.x * (32 * SG_EPI_WARPS);
+    for (int64_t i = me; i < p0; i += all) out[i] = T(0.f);
+    for (int64_t i = p1 + me; i < end; i += all) out[i] = T(0.f);
+}
+
 // 32 accumulator columns of this warp's 32 rows
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
     tmem_ld16(taddr, r);
     tmem_ld16(taddr + 16, r + 16);
 }
 
-template <int MODE, int LEVELS, typename T>
+template <int MODE, typename T>
 __global__ void __launch_bounds__(SG_THREADS, 1)
 segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const SegGemmParams P) {
-    extern __shared__ unsigned char smem_raw[];
+    extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzle atoms lie on 1024 bytes
     __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 4];  // full[S], empty[S], acc_full[2], acc_empty[2]
+    __shared__ __align__(16) float s_cols[MODE == SG_I8 ? 2 : 1][256];                 // bias and column scales of the tile, zeros past the last
     __shared__ uint32_t tmem_base_slot;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int S = P.stages, bn = P.bn;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t base = smem_u32(smem_raw);
+    if (base & 1023u) {  // (never: the array's own alignment)
+        if (tid == 0) atomicExch(P.status, 7);
+        return;
+    }
     const uint32_t b_bytes = (uint32_t)bn * 128u;
-    const uint32_t slot_bytes = (uint32_t)LEVELS * (SG_A_BYTES + b_bytes);
+    const uint32_t slot_bytes = SG_A_BYTES + b_bytes;
     const uint32_t stage0 = base, ring0 = base + SG_EPI_WARPS * SG_STAGING;
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
@@ -208,29 +239,10 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     pdl_wait_exclusive();
     if (P.reset && blockIdx.x == 0 && tid == 0) *P.status = 0;
     const uint32_t tmem_base = tmem_base_slot;
-    const uint32_t acc_cols = (uint32_t)(LEVELS == 3 ? 2 * bn : bn);
+    const uint32_t acc_cols = (uint32_t)bn;
     bool failed = false;
 
-    // every role walks the same pieces of work: body(rows of one segment, block of features, block of columns, part) until it says stop
-    auto walk = [&](auto body) {
-        for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
-            const int n = (int)(u % P.tiles_n);
-            if constexpr (MODE != SG_DW) {
-                const SegRows t = seg_tile(P, u / P.tiles_n);
-                if (t.hi > t.lo && !body(t, 0, n, (int64_t)0)) return;
-            } else {
-                const int64_t v = u / P.tiles_n, part = v / P.tiles_m;
-                const int64_t r0 = part * P.part_rows, r1 = r0 + P.part_rows < P.N ? r0 + P.part_rows : P.N;
-                int g = last_segment(P.G, [&](int q) { return seg_at(P, q) <= r0; });
-                for (g = g < 0 ? 0 : g; g < P.G; ++g) {
-                    const int64_t a = seg_at(P, g), b = seg_at(P, g + 1);
-                    if (a >= r1) break;
-                    const SegRows t = {a > r0 ? a : r0, b < r1 ? b : r1, g};
-                    if (t.hi > t.lo && !body(t, (int)(v % P.tiles_m), n, part)) return;
-                }
-            }
-        }
-    };
+    auto walk = [&](auto body) { sg_walk<MODE>(P, body); };
     auto slices_of = [&](const SegRows& t) { return MODE == SG_DW ? (int)((t.hi - t.lo + 63) >> 6) : P.slices; };
 
     if (warp == 0) {
@@ -245,23 +257,19 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                 if (lane == 0) {
                     ok = mbar_wait_bounded(empty(s), ((it / (uint32_t)S) & 1u) ^ 1u);
                     if (ok) {
-                        mbar_arrive_expect_tx(full(s), (uint32_t)LEVELS * (a_box + b_bytes));
-                        const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + LEVELS * SG_A_BYTES;
-#pragma unroll
-                        for (int l = 0; l < LEVELS; ++l) {
-                            const uint32_t al = a0 + (uint32_t)l * SG_A_BYTES, bl = b0 + (uint32_t)l * b_bytes;
-                            if constexpr (MODE == SG_DW) {
-                                const int row = (int)(t.lo + (int64_t)j * 64);
-                                for (int h = 0; h < 2; ++h) sg_load(al + (uint32_t)h * 8192u, &mapA, mb * 128 + h * 64, row, l, full(s), once);
-                                for (int h = 0; h < bn / 64; ++h) sg_load(bl + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, l, full(s), once);
-                            } else {
-                                constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
-                                sg_load(al, &mapA, j * STEP, (int)t.lo, l, full(s), once);
-                                if constexpr (MODE == SG_Y)
-                                    for (int h = 0; h < bn / 64; ++h) sg_load(bl + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, l * P.G + t.g, full(s), keep);
-                                else
-                                    sg_load(bl, &mapB, j * STEP, nb * bn, l * P.G + t.g, full(s), keep);
-                            }
+                        mbar_arrive_expect_tx(full(s), a_box + b_bytes);
+                        const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
+                        if constexpr (MODE == SG_DW) {
+                            const int row = (int)(t.lo + (int64_t)j * 64);
+                            for (int h = 0; h < 2; ++h) sg_load(a0 + (uint32_t)h * 8192u, &mapA, mb * 128 + h * 64, row, 0, full(s), once);
+                            for (int h = 0; h < bn / 64; ++h) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, 0, full(s), once);
+                        } else {
+                            constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
+                            sg_load(a0, &mapA, j * STEP, (int)t.lo, 0, full(s), once);
+                            if constexpr (MODE == SG_Y)
+                                for (int h = 0; h < bn / 64; ++h) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, t.g, full(s), keep);
+                            else
+                                sg_load(b0, &mapB, j * STEP, nb * bn, t.g, full(s), keep);
                         }
                     }
                 }
@@ -284,14 +292,14 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             bool ok = lane != 0 || mbar_wait_bounded(acc_empty(a), ((lt >> 1) & 1u) ^ 1u);
             for (int j = 0; j < slices; ++j, ++it) {
                 const int s = (int)(it % (uint32_t)S);
-                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + LEVELS * SG_A_BYTES;
+                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
                 if (lane == 0 && ok) ok = mbar_wait_bounded(full(s), (it / (uint32_t)S) & 1u);
                 if (!__shfl_sync(0xFFFFFFFFu, (int)ok, 0)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {
                     const int have = (int)(t.hi - t.lo - (int64_t)j * 64);
                     if (have < 64) {  // rows of the next segment: 128 bytes each, from `have` to the end of every box
                         mbar_wait_bounded(full(s), (it / (uint32_t)S) & 1u);  // (has completed: orders every lane's stores behind the copies)
-                        for (int box = 0; box < LEVELS * (2 + bn / 64); ++box)
+                        for (int box = 0; box < 2 + bn / 64; ++box)
                             for (uint32_t o = (uint32_t)have * 128u + (uint32_t)lane * 16u; o < 8192u; o += 512u)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a0 + (uint32_t)box * 8192u + o), "r"(0u) : "memory");
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -302,20 +310,15 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-#pragma unroll
-                        for (int q = (LEVELS == 3 ? 0 : 5); q < 6; ++q) {
-                            const uint32_t al = a0 + sg_pair_a(q) * SG_A_BYTES, bl = b0 + sg_pair_b(q) * b_bytes;
-                            // K-major: rows 128 bytes apart, groups of 8 rows 1024, a k-step 32 bytes along the row.  MN-major: 16
-                            // contraction rows of 128 bytes a k-step, boxes of 64 columns 8192 bytes apart
-                            const uint64_t ad = MODE == SG_DW ? make_smem_desc(al + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
-                                                              : make_smem_desc(al + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
-                            const uint64_t bd = MODE == SG_DW || MODE == SG_Y ? make_smem_desc(bl + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
-                                                                              : make_smem_desc(bl + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
-                            const bool first = j == 0 && kk == 0 && (q == 5 || q == 0);
-                            const uint32_t to = dacc + (LEVELS == 3 && q < 5 ? (uint32_t)bn : 0u);
-                            if constexpr (MODE == SG_I8) mma_i8_ss(to, ad, bd, idesc, first ? 0u : 1u);
-                            else mma_bf16_ss(to, ad, bd, idesc, first ? 0u : 1u);
-                        }
+                        // K-major: rows 128 bytes apart, groups of 8 rows 1024, a k-step 32 bytes along the row.  MN-major: 16
+                        // contraction rows of 128 bytes a k-step, boxes of 64 columns 8192 bytes apart
+                        const uint64_t ad = MODE == SG_DW ? make_smem_desc(a0 + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
+                                                          : make_smem_desc(a0 + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
+                        const uint64_t bd = MODE == SG_DW || MODE == SG_Y ? make_smem_desc(b0 + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
+                                                                          : make_smem_desc(b0 + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
+                        const uint32_t more = j > 0 || kk > 0;
+                        if constexpr (MODE == SG_I8) mma_i8_ss(dacc, ad, bd, idesc, more);
+                        else mma_bf16_ss(dacc, ad, bd, idesc, more);
                     }
                     mma_commit(empty(s));
                 }
@@ -329,8 +332,18 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         const int ew = warp - 2, quarter = warp & 3, half = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
         uint32_t lt = 0;
+        int staged_g = -1, staged_n = -1;
         walk([&](const SegRows& t, int mb, int nb, int64_t part) {
             const uint32_t a = lt & 1u;
+            if (MODE != SG_DW && (P.bias || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
+                const int c = tid - 64, col = nb * bn + c;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                s_cols[0][c] = P.bias && c < bn && col < P.cols_out ? P.bias[(int64_t)t.g * P.cols_out + col] : 0.f;
+                if constexpr (MODE == SG_I8) s_cols[1][c] = c < bn && col < P.cols_out ? P.sw[col] : 0.f;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                staged_g = t.g;
+                staged_n = nb;
+            }
             if (!mbar_wait_bounded(acc_full(a), (lt >> 1) & 1u)) { failed = true; return false; }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
@@ -344,25 +357,22 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             auto fetch = [&](int c, float* f) {
                 uint32_t r[32];
                 tmem_ld32(taddr + (uint32_t)c, r);
-                if constexpr (LEVELS == 3) {
-                    uint32_t m[32];
-                    tmem_ld32(taddr + (uint32_t)(bn + c), m);
-                    tmem_ld_wait();
+                tmem_ld_wait();
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) f[q] = __uint_as_float(r[q]) + __uint_as_float(m[q]);
-                } else {
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) f[q] = MODE == SG_I8 ? (float)(int)r[q] : __uint_as_float(r[q]);
-                }
+                for (int q = 0; q < 32; ++q) f[q] = MODE == SG_I8 ? (float)(int)r[q] : __uint_as_float(r[q]);
                 if constexpr (MODE == SG_I8) {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) f[q] *= sx * (c_base + c + q < c_end ? P.sw[c_base + c + q] : 0.f);
+                    for (int q = 0; q < 32; q += 4) {
+                        const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c + q]);
+                        f[q] *= sx * w.x; f[q + 1] *= sx * w.y; f[q + 2] *= sx * w.z; f[q + 3] *= sx * w.w;
+                    }
                 }
                 if (MODE != SG_DW && P.bias) {
-                    const float* b = P.bias + (int64_t)t.g * P.cols_out + c_base + c;
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) f[q] += c_base + c + q < c_end ? b[q] : 0.f;
+                    for (int q = 0; q < 32; q += 4) {
+                        const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
+                        f[q] += b.x; f[q + 1] += b.y; f[q + 2] += b.z; f[q + 3] += b.w;
+                    }
                 }
                 if (MODE != SG_DW && P.relu) {
 #pragma unroll
@@ -409,13 +419,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             ++lt;
             return true;
         });
-        if (MODE == SG_Y || MODE == SG_DX) {  // rows of no segment: zeros
-            const int64_t p0 = seg_at(P, 0) * P.cols_out, p1 = seg_at(P, P.G) * P.cols_out, end = P.N * P.cols_out;
-            T* const out = (T*)P.out;
-            const int64_t me = (int64_t)blockIdx.x * (32 * SG_EPI_WARPS) + (tid - 64), all = (int64_t)gridDim.x * (32 * SG_EPI_WARPS);
-            for (int64_t i = me; i < p0; i += all) out[i] = T(0.f);
-            for (int64_t i = p1 + me; i < end; i += all) out[i] = T(0.f);
-        }
+        if (MODE == SG_Y || MODE == SG_DX) sg_zero_outside(P, (T*)P.out);
     }
     if (failed) atomicExch(P.status, 7);  // GNN_ERR_TIMEOUT
     tc_fence_before();
@@ -425,8 +429,11 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
 // [planes, rows, cols] of bf16 (or bytes), rows ld elements apart, planes directly after one another; box = 128 bytes x box_rows
 // rows of one plane, swizzled; out-of-range reads give zeros (linear_tma.cu)
-bool make_map_planes(CUtensorMap* m, const void* ptr, bool bytes, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int box_rows);
+// type: 0 bf16, 1 bytes, 2 fp32
+bool make_map_planes(CUtensorMap* m, const void* ptr, int type, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 bool tensor_map_encoder_available();
+// SG_Y, SG_DX or SG_DW of fp32 (segment_gemm_f32.cu); slot: of allow_big_smem
+gnn_status segment_gemm_f32(const char* who, int mode, int slot, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st);
 
 // output columns of a tile: as few blocks of at most `most` as cover them, evened out, in steps of 64; halved while there are
 // fewer tiles than SMs (a tile's weights then arrive through more SMs)
@@ -437,16 +444,16 @@ inline int sg_block(int cols, int most, int64_t row_tiles) {
     return bn;
 }
 
-template <int MODE, int LEVELS, typename T>
+template <int MODE, typename T>
 static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st) {
-    const auto kernel = segment_gemm_kernel<MODE, LEVELS, T>;
+    const auto kernel = segment_gemm_kernel<MODE, T>;
     const gnn_status rc = allow_big_smem(who, (const void*)kernel, which, SG_SMEM_MAX);
     if (rc != GNN_OK) return rc;
-    const size_t fixed = 1024 + SG_EPI_WARPS * SG_STAGING, slot = (size_t)LEVELS * (SG_A_BYTES + (size_t)P.bn * 128);
+    const size_t fixed = SG_EPI_WARPS * SG_STAGING, slot = SG_A_BYTES + (size_t)P.bn * 128;
     int stages = (int)((SG_SMEM_MAX - fixed) / slot);
     P.stages = stages > SG_MAX_STAGES ? SG_MAX_STAGES : stages;
     int cols = 32;
-    while (cols < 2 * P.bn * (LEVELS == 3 ? 2 : 1)) cols <<= 1;
+    while (cols < 2 * P.bn) cols <<= 1;
     P.tmem_cols = cols;
     launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SG_THREADS), fixed + (size_t)P.stages * slot, st, mapA, mapB, P);
     GNN_CHECK_LAUNCH(who);
