@@ -10,54 +10,78 @@ constexpr int I8_SLOT = 54;  // of allow_big_smem: two of them
 
 // ------------------------------------------------------------------ rows to 8 bits
 // scale = max |x| / 127, q = x / scale rounded to the nearest integer, ties to even, as the exact quotient would be: the
-// estimate x * (1 / scale) is off by less than 1e-4, and what remains, x - q * scale, is exact in fp32 (a multiple of the
-// last bit of scale, or of half of it where q is 1, and at most about half of scale), so one comparison with scale / 2 finds
-// the neighbour where the estimate fell on the wrong side.
-__device__ __forceinline__ int round_quotient(float x, float inv, float scale) {
-    float q = rintf(x * inv);
-    const float r = 2.f * fmaf(-q, scale, x);
-    const float a = fabsf(r);
-    if (a >= scale) {  // rare
-        const bool odd = ((int)q & 1) != 0;
-        if (a > scale || odd) q += r > 0.f ? 1.f : -1.f;
-    }
-    return (int)q;
-}
+// estimate, x * (1 / scale) rounded by adding 1.5 * 2^23 (one fma; the integer is in the sum's low bits), is off by less than 1e-4
+// of a step, and what remains, r = x - q * scale, is exact in fp32 (a multiple of the last bit of scale, or of half of it where
+// q is 1, and at most about half of scale).  Where 2 |r| is under scale, q stands; the few chunks with a value at or beyond the
+// half are done again with care.
+constexpr float Q_MAGIC = 12582912.f;
 
 struct RowScale {
-    float scale, inv, s, up;
+    float scale, inv;
     // from the bits of max |x|: not finite -> scale NaN and zeros; scale 0 (or underflown to it) -> zeros
     __device__ __forceinline__ explicit RowScale(uint32_t top) {
         scale = top < 0x7F800000u ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7FC00000u);
-        // 1 / scale would overflow: the same quotient of values 2^80 times as large (exact)
-        up = scale < 1e-30f ? 1.2089258196146292e24f : 1.f;
-        s = scale * up;
-        inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;  // NaN and 0: all zeros
-        if (!(s > 0.f)) up = 0.f;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));  // 2^-23 of it off: of 127 steps, 2e-5 of a step
     }
-    __device__ __forceinline__ int operator()(float x) const { return up == 0.f ? 0 : round_quotient(x * up, inv, s); }
+    __device__ __forceinline__ bool zeros() const { return !(scale > 0.f); }  // NaN too
+    __device__ __forceinline__ bool tiny() const { return scale < 1e-30f; }    // 1 / scale may overflow
+    __device__ __forceinline__ float estimate(float x) const { return fmaf(x, inv, Q_MAGIC); }
+    // what the estimate leaves, at most half of scale where it is right
+    __device__ __forceinline__ float rest(float x, float e) const { return fabsf(fmaf(-(e - Q_MAGIC), scale, x)); }
+    // with care: the neighbour where the remainder passes half a step, the even one where it is half a step
+    __device__ __forceinline__ int exact(float x) const {
+        float s = scale, i = inv;
+        if (tiny()) {  // the same quotient of values 2^80 times as large (exact)
+            x *= 1.2089258196146292e24f;
+            s *= 1.2089258196146292e24f;
+            i = __fdiv_rn(1.f, s);
+        }
+        float q = fmaf(x, i, Q_MAGIC) - Q_MAGIC;
+        const float r = 2.f * fmaf(-q, s, x), a = fabsf(r);
+        if (a > s || (a == s && ((int)q & 1))) q += r > 0.f ? 1.f : -1.f;
+        return (int)q;
+    }
 };
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
+// largest |x| of a chunk, as bits that order as the values do (what is not finite above all)
 template <typename T>
 __device__ __forceinline__ uint32_t chunk_top(uint4 v) {
-    float f[Chunk<T>::N];
-    Chunk<T>::unpack(v, f);
     uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < Chunk<T>::N; ++k) m = max(m, abs_bits(f[k]));
+    if constexpr (Chunk<T>::N == 4) {
+        m = max(max(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), max(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
+    } else {  // two bf16 to a word, compared as 16-bit integers
+        const uint32_t a = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+        m = max(a << 16, a & 0xFFFF0000u);
+    }
     return m;
 }
 template <typename T>
 __device__ __forceinline__ void chunk_out(uint4 v, const RowScale& rs, int8_t* q) {
-    float f[Chunk<T>::N];
-    Chunk<T>::unpack(v, f);
-    uint32_t w[Chunk<T>::N / 4];
+    constexpr int N = Chunk<T>::N;
+    uint32_t w[N / 4];
+    if (rs.zeros()) {
 #pragma unroll
-    for (int k = 0; k < Chunk<T>::N / 4; ++k)
-        w[k] = (uint32_t)(rs(f[4 * k]) & 0xFF) | (uint32_t)(rs(f[4 * k + 1]) & 0xFF) << 8 | (uint32_t)(rs(f[4 * k + 2]) & 0xFF) << 16 | (uint32_t)(rs(f[4 * k + 3]) & 0xFF) << 24;
-    if constexpr (Chunk<T>::N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+        for (int k = 0; k < N / 4; ++k) w[k] = 0;
+    } else {
+        float f[N], far = 0.f;
+        uint32_t u[N];
+        Chunk<T>::unpack(v, f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float e = rs.estimate(f[k]);
+            u[k] = __float_as_uint(e);
+            far = fmaxf(far, rs.rest(f[k], e));
+        }
+        if (2.f * far >= rs.scale || rs.tiny()) {  // rare
+#pragma unroll
+            for (int k = 0; k < N; ++k) u[k] = (uint32_t)rs.exact(f[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) w[k] = __byte_perm(__byte_perm(u[4 * k], u[4 * k + 1], 0x0040), __byte_perm(u[4 * k + 2], u[4 * k + 3], 0x0040), 0x5410);
+    }
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(q) = w[0];
 }
 
@@ -90,6 +114,41 @@ quantize_rows_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float
         if (lane + c * L < chunks) chunk_out<T>(v[c], rs, q + row * K + (lane + c * L) * PER);
 }
 
+// long rows: a block per row, CH chunks per thread in registers
+template <typename T, int CH>
+__global__ void __launch_bounds__(256)
+quantize_long_rows_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
+    pdl_wait();
+    __shared__ uint32_t tops[2][8];
+    constexpr int PER = Chunk<T>::N;
+    const int chunks = K / PER;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < N; row += gridDim.x, turn ^= 1) {
+        const T* const x = X + row * K;
+        uint4 v[CH];
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int i = (int)threadIdx.x + c * 256;
+            v[c] = i < chunks ? ld_16(x + i * PER) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) top = max(top, chunk_top<T>(v[c]));
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if (threadIdx.x % 32 == 0) tops[turn][threadIdx.x / 32] = top;
+        __syncthreads();  // the other half of tops serves the next row: one barrier a row
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = max(top, tops[turn][w]);
+        const RowScale rs(top);
+        if (threadIdx.x == 0) scale[row] = rs.scale;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int i = (int)threadIdx.x + c * 256;
+            if (i < chunks) chunk_out<T>(v[c], rs, q + row * K + i * PER);
+        }
+    }
+}
+
 // any K: a block per row, elements one by one, read twice
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -108,7 +167,7 @@ quantize_any_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float*
         __syncthreads();
         const RowScale rs(top);
         if (threadIdx.x == 0) scale[row] = rs.scale;
-        for (int k = threadIdx.x; k < K; k += 256) q[row * K + k] = (int8_t)rs((float)x[k]);
+        for (int k = threadIdx.x; k < K; k += 256) q[row * K + k] = rs.zeros() ? (int8_t)0 : (int8_t)rs.exact((float)x[k]);
     }
 }
 
@@ -117,15 +176,23 @@ static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scal
     constexpr int PER = Chunk<T>::N;
     const int chunks = K / PER;
     auto run = [&](auto kernel, int lanes) { launch_overlapped(kernel, dim3((unsigned)ceil_div(N * lanes, 256)), dim3(256), 0, st, X, N, K, q, scale); };
-    if (K % PER != 0 || chunks > 256) {
-        launch_overlapped(quantize_any_kernel<T>, dim3((unsigned)(N < 148 * 8 ? N : 148 * 8)), dim3(256), 0, st, X, N, K, q, scale);
+    const dim3 rows((unsigned)(N < 148 * 8 ? N : 148 * 8));
+    if (K % PER == 0 && chunks > 256 && chunks <= 2048) {
+        auto run_long = [&](auto kernel) { launch_overlapped(kernel, rows, dim3(256), 0, st, X, N, K, q, scale); };
+        chunks <= 512 ? run_long(quantize_long_rows_kernel<T, 2>) : chunks <= 1024 ? run_long(quantize_long_rows_kernel<T, 4>) : run_long(quantize_long_rows_kernel<T, 8>);
         return;
     }
+    if (K % PER != 0 || chunks > 2048) {
+        launch_overlapped(quantize_any_kernel<T>, rows, dim3(256), 0, st, X, N, K, q, scale);
+        return;
+    }
+    // four chunks per lane where the row has them: what a row costs once (the scale, the maximum over its lanes) is shared by 32 values
+    // (170,000 x 256 bf16, two chunks per lane: 33.7 us)
     if (chunks <= 4) run(quantize_rows_kernel<T, 4, 1>, 4);
     else if (chunks <= 8) run(quantize_rows_kernel<T, 4, 2>, 4);
-    else if (chunks <= 16) run(quantize_rows_kernel<T, 8, 2>, 8);
-    else if (chunks <= 32) run(quantize_rows_kernel<T, 16, 2>, 16);
-    else if (chunks <= 64) run(quantize_rows_kernel<T, 32, 2>, 32);
+    else if (chunks <= 16) run(quantize_rows_kernel<T, 4, 4>, 4);
+    else if (chunks <= 32) run(quantize_rows_kernel<T, 8, 4>, 8);
+    else if (chunks <= 64) run(quantize_rows_kernel<T, 16, 4>, 16);
     else if (chunks <= 128) run(quantize_rows_kernel<T, 32, 4>, 32);
     else run(quantize_rows_kernel<T, 32, 8>, 32);
 }

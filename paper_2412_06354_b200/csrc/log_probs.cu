@@ -118,6 +118,61 @@ __device__ __forceinline__ uint64_t lp_best_of(const uint64_t* keys, int n, int 
     return best;
 }
 
+// Running sums of one thread: r = m log2(e) rounded, s = sum of 2^(z log2(e) - r) over all of its classes, t the same weighted by the
+// exponent.  Two classes at a time (packed fp32 instructions).  z log2(e) - r is one rounding off whatever m is; what r itself is off
+// by is taken out at the end.  Beyond |m| = 1e37, where m log2(e) could overflow, neighbouring numbers are 1e30 apart: 2^(z / 4 - m / 4)
+// tells as well who is at m, and all others are 0.
+struct LpRun {
+    float m, r, k;
+    float2 s, t;
+    static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+    __device__ __forceinline__ void clear() { m = -INFINITY; r = 0.f; k = LOG2E; s = t = make_float2(0.f, 0.f); }
+    static __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+        float2 d;
+        asm("{.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;}"
+            : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+        return d;
+    }
+    static __device__ __forceinline__ float2 add2(float2 a, float2 b) {
+        float2 d;
+        asm("{.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;}"
+            : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+        return d;
+    }
+    static __device__ __forceinline__ float exp2_(float u) {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u));
+        return e;
+    }
+    // the maximum becomes v > m
+    __device__ __forceinline__ void raise(float v) {
+        const bool first = m == -INFINITY;
+        k = fabsf(v) > 1e37f ? 0.25f : LOG2E;
+        const float q = v * k, d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
+        t = first ? make_float2(0.f, 0.f) : make_float2(f * fmaf(d, s.x, t.x), f * fmaf(d, s.y, t.y));
+        s = make_float2(f * s.x, f * s.y);  // (not a number stays one)
+        m = v;
+        r = q;
+    }
+    // two scores, neither above m; -inf: 2^-inf = 0 times a finite exponent
+    __device__ __forceinline__ void add(float a, float b) {
+        const float2 u = fma2(make_float2(a, b), make_float2(k, k), make_float2(-r, -r));
+        const float2 e = make_float2(exp2_(u.x), exp2_(u.y));
+        s = add2(s, e);
+        t = fma2(e, make_float2(fmaxf(u.x, -2000.f), fmaxf(u.y, -2000.f)), t);
+    }
+    __device__ __forceinline__ LpStats stats() const {
+        LpStats o;
+        const float S = s.x + s.y;
+        o.m = m;
+        if (!(m > -INFINITY) || m == INFINITY) { o.s = S == S && m < INFINITY ? 0.f : __uint_as_float(0x7FC00000u); o.t = 0.f; return o; }
+        const float off = fmaf(m, k, -r), f = exp2_(-off);
+        o.s = fmaf(f, S, -1.f);
+        o.t = LN2 * f * fmaf(-off, S, t.x + t.y);
+        return o;
+    }
+};
+
 struct LpParams {
     const void* z;
     const int32_t* label;  // or nullptr
@@ -169,23 +224,31 @@ log_probs_few_kernel(const LpParams P) {
     const int rows = (int)(P.N - r0 < LP_ROWS ? P.N - r0 : LP_ROWS);
     const T* const z = (const T*)P.z + r0 * C;  // on 16 bytes: LP_ROWS rows are
     const int elements = rows * C;
-    for (int e = (int)threadIdx.x * PER; e < elements; e += LP_ROWS * PER) {
-        float f[PER];
-        if (e + PER <= elements) Chunk<T>::unpack(ld_16(z + e), f);
-        else
+    {
+        int r = (int)threadIdx.x * PER / C, c = (int)threadIdx.x * PER - r * C;
+        const int dr = LP_ROWS * PER / C, dc = LP_ROWS * PER - dr * C;
+        for (int e = (int)threadIdx.x * PER; e < elements; e += LP_ROWS * PER) {
+            float f[PER];
+            if (e + PER <= elements) Chunk<T>::unpack(ld_16(z + e), f);
+            else
 #pragma unroll
-            for (int k = 0; k < PER; ++k) f[k] = e + k < elements ? (float)z[e + k] : 0.f;
-        int r = (int)((unsigned)e / (unsigned)C), c = e - r * C;
+                for (int k = 0; k < PER; ++k) f[k] = e + k < elements ? (float)z[e + k] : 0.f;
+            int at = r * stride + c, left = C - c;  // to the end of the row
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            if (e + k < elements) sh_z[r * stride + c] = f[k];
-            if (++c == C) { c = 0; ++r; }
+            for (int k = 0; k < PER; ++k) {
+                if (e + k < elements) sh_z[at] = f[k];
+                ++at;
+                if (--left == 0) { left = C; at += stride - C; }
+            }
+            r += dr;
+            c += dc;
+            if (c >= C) { c -= C; ++r; }
         }
     }
     __syncthreads();
     if ((int)threadIdx.x >= rows) return;
     const int64_t row = r0 + threadIdx.x;
-    const float* const mine = sh_z + threadIdx.x * stride;
+    float* const mine = sh_z + threadIdx.x * stride;
     const float nan = __uint_as_float(0x7FC00000u);
     float v[CM];
 #pragma unroll
@@ -224,25 +287,59 @@ log_probs_few_kernel(const LpParams P) {
         const int y = P.label[row];
         P.logp[row] = y >= 0 && y < C ? logp(mine[y]) : 0.f;
     }
-    float m = st.m;
-    int at = lead;
+    // The best: the largest of the groups' largest scores (eight classes each), then its group again in shared memory, where what is
+    // taken becomes NaN.  (All CM scores in registers looked through for every class listed: 29 us instead of XX.)
+    float gm[CM / 8];
+#pragma unroll
+    for (int g = 0; g < CM / 8; ++g) {
+        gm[g] = v[8 * g];
+#pragma unroll
+        for (int c = 1; c < 8; ++c) gm[g] = fmaxf(gm[g], v[8 * g + c]);
+    }
     for (int j = 0; j < P.top; ++j) {
-        if (j > 0) {
-            m = largest();
-            at = where(m);
-        }
-        if (at >= C) {  // numbers are used up: what is not one, in order
-            int skip = j;  // classes listed so far that are not numbers: all but the numbers before
-            for (int c = 0; c < C; ++c) skip -= mine[c] == mine[c];
-            if (skip < 0) skip = 0;
+        float m = gm[0];
+#pragma unroll
+        for (int g = 1; g < CM / 8; ++g) m = fmaxf(m, gm[g]);
+        int first = CM / 8;
+#pragma unroll
+        for (int g = CM / 8 - 1; g >= 0; --g) first = gm[g] == m ? g : first;
+        int at = C;
+        if (first < CM / 8) {
+            float next = nan;
+#pragma unroll
+            for (int c = 7; c >= 0; --c) {
+                const float x = 8 * first + c < C ? mine[8 * first + c] : nan;
+                if (x == m) {
+                    next = at < C ? m : next;  // the one after it stays, an equal
+                    at = 8 * first + c;
+                } else {
+                    next = fmaxf(next, x);
+                }
+            }
+            mine[at] = nan;
+#pragma unroll
+            for (int g = 0; g < CM / 8; ++g) gm[g] = g == first ? next : gm[g];
+        } else {  // numbers are used up: what is not one, in order
+            int skip = j;
+            for (int c = 0; c < C; ++c) skip -= !((float)z[threadIdx.x * C + c] != (float)z[threadIdx.x * C + c]);
             for (int c = 0; c < C; ++c)
-                if (mine[c] != mine[c] && skip-- == 0) at = c;
+                if ((float)z[threadIdx.x * C + c] != (float)z[threadIdx.x * C + c] && skip-- == 0) at = c;
             m = nan;
         }
         P.top_idx[row * P.top + j] = at;
         P.top_logp[row * P.top + j] = logp(m);
+    }
+}
+
+// the statistics of a warp's lanes, in the same order for both sides of a pair
+__device__ __forceinline__ void lp_join_lanes(LpStats& st, int lane) {
 #pragma unroll
-        for (int c = 0; c < CM; ++c) v[c] = c == at ? nan : v[c];
+    for (int o = 16; o > 0; o >>= 1) {
+        LpStats q;
+        q.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, o);
+        q.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, o);
+        q.t = __shfl_xor_sync(0xFFFFFFFFu, st.t, o);
+        if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
     }
 }
 
@@ -265,7 +362,7 @@ log_probs_kernel(const LpParams P) {
     __shared__ uint64_t sh_cand[W == 1 ? 8 : 1][LP_CAND];
     __shared__ uint64_t sh_keys[W == 1 ? 1 : 8][LP_TOP];
     __shared__ float sh_sorted[W == 1 ? 1 : 8][32], sh_floor;
-    __shared__ int sh_count[8];
+    __shared__ int sh_count[8], sh_owner;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + warp : (int64_t)blockIdx.x / P.parts;
     const int part = W == 1 ? 0 : (int)(blockIdx.x % P.parts);
@@ -290,9 +387,8 @@ log_probs_kernel(const LpParams P) {
         return x.q;
     };
     auto inside = [&](int64_t i, int k) { return i * PER + k >= e0 && i * PER + k < e1; };
-    LpStats st;
-    st.clear();
-    float mine = -INFINITY;
+    LpRun run;
+    run.clear();
     const bool list = P.top > 0;
     constexpr int U = 4;  // chunks in flight per lane
     int n = 0;
@@ -321,31 +417,77 @@ log_probs_kernel(const LpParams P) {
                 sh_max[n * 256 + threadIdx.x] = cm;
                 ++n;
             }
-            if (cm > st.m) {
-                st.raise(cm);
-                bool taken = false;
+            if (cm > run.m) run.raise(cm);
 #pragma unroll
-                for (int k = 0; k < PER; ++k) {
-                    const bool skip = !taken && f[k] == cm;
-                    taken |= skip;
-                    if (!skip) st.add(f[k], cm);
-                }
-            } else {
-                const float base = st.m == -INFINITY ? 0.f : st.m;
-#pragma unroll
-                for (int k = 0; k < PER; ++k) st.add(f[k], base);
-            }
+            for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
         }
     }
-    mine = st.m;  // its own largest score
+    const float mine = run.m;  // its own largest score
+    LpStats st = run.stats();
+    lp_join_lanes(st, lane);
+    if constexpr (W > 1) {
+        if (lane == 0) sh_stats[warp] = st;
+        __syncthreads();
+        st = sh_stats[0];
+        for (int w = 1; w < W; ++w) st.join(sh_stats[w]);  // all warps alike
+    }
+    // One class takes most of it: the sum beside its own 1 has lost digits in the thread that holds it.  That thread's chunks again,
+    // without the 1, by its warp; the other threads' sums stand.
+    if (st.s < 2.f && st.m > -INFINITY && st.m < INFINITY) {
+        const uint32_t at = __ballot_sync(0xFFFFFFFFu, mine == st.m);
+        int owner = at ? warp * 32 + __ffs(at) - 1 : 256;
+        if constexpr (W > 1) {
+            if (threadIdx.x == 0) sh_owner = 256;
+            __syncthreads();
+            if (lane == 0) atomicMin(&sh_owner, owner);
+            __syncthreads();
+            owner = sh_owner;
+        }
+        LpStats own = run.stats();
+        if (owner / 32 == warp) {
+            const int who = W == 1 ? owner % 32 : owner;
+            LpStats again;
+            again.clear();
+            again.m = st.m;
+            bool taken = false;  // the first of its classes at the maximum
+            for (int64_t c = c0 + who; c < c1; c += 32 * STEP) {
+                const int64_t i = c + (int64_t)lane * STEP;
+                float f[PER];
+                bool hit = false;
+                if (i < c1) {
+                    Chunk<T>::unpack(load(i), f);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        LpStats q;
-        q.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, o);
-        q.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, o);
-        q.t = __shfl_xor_sync(0xFFFFFFFFu, st.t, o);
-        // both sides of a pair join in the same order
-        if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
+                    for (int k = 0; k < PER; ++k) {
+                        if (!inside(i, k)) f[k] = -INFINITY;
+                        hit |= f[k] == st.m;
+                    }
+                }
+                const uint32_t hits = __ballot_sync(0xFFFFFFFFu, hit);
+                bool skip = !taken && hits && lane == __ffs(hits) - 1;
+                taken |= hits != 0;
+                if (i < c1) {
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) {
+                        if (skip && f[k] == st.m) skip = false;
+                        else again.add(f[k], st.m);
+                    }
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                again.s += __shfl_xor_sync(0xFFFFFFFFu, again.s, o);
+                again.t += __shfl_xor_sync(0xFFFFFFFFu, again.t, o);
+            }
+            if (lane == owner % 32) own = again;
+        }
+        st = own;
+        lp_join_lanes(st, lane);
+        if constexpr (W > 1) {
+            if (lane == 0) sh_stats[warp] = st;
+            __syncthreads();
+            st = sh_stats[0];
+            for (int w = 1; w < W; ++w) st.join(sh_stats[w]);
+        }
     }
     uint64_t best = 0;
     if (list) {
@@ -401,10 +543,7 @@ log_probs_kernel(const LpParams P) {
         }
     }
     if constexpr (W > 1) {
-        if (lane == 0) sh_stats[warp] = st;
-        __syncthreads();
         if (warp != 0) return;
-        for (int w = 1; w < W; ++w) st.join(sh_stats[w]);
         if (P.parts > 1) {
             const int64_t at = row * P.parts + part;
             if (lane == 0) { P.stats[at * 4] = st.m; P.stats[at * 4 + 1] = st.s; P.stats[at * 4 + 2] = st.t; }
@@ -440,14 +579,7 @@ log_probs_join_kernel(const LpParams P) {
         }
         if (P.top > 0) top = lp_merge(top, lp_sort(k, lane), lane);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        LpStats q;
-        q.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, o);
-        q.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, o);
-        q.t = __shfl_xor_sync(0xFFFFFFFFu, st.t, o);
-        if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
-    }
+    lp_join_lanes(st, lane);
     if (lane == 0) sh_stats[warp] = st;
     sh_keys[warp][lane] = top;
     if (threadIdx.x == 0) sh_count = 0;
@@ -591,11 +723,11 @@ log_probs_backward_kernel(const LpGradParams P) {
     }
 }
 
-// Blocks per row: as many as give the SMs eight blocks each while every block has 8 KB of the row at least; and enough that a
+// Blocks per row: as many as give the SMs twelve blocks each while every block has 8 KB of the row at least; and enough that a
 // thread has LP_CHUNKS chunks at most.
 static int64_t lp_parts(int64_t N, int64_t C, int s) {
     const int64_t bytes = C * s, least = ceil_div(bytes + 16, (int64_t)LP_CHUNKS * 256 * 16 - 16);
-    int64_t p = N < 148 * 4 ? (148 * 8) / N : 1;
+    int64_t p = N < 148 * 4 ? (148 * 12) / N : 1;
     const int64_t most = bytes / (8 * 1024);
     p = p < most ? p : most;
     return p > least ? p : least;
