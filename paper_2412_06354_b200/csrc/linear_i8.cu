@@ -17,17 +17,17 @@ constexpr int I8_SLOT = 54;  // of allow_big_smem: two of them
 constexpr float Q_MAGIC = 12582912.f;
 
 struct RowScale {
-    float scale, inv;
+    float scale, inv, half, start;  // start: where the remainders' maximum begins (above half: all with care)
+    uint32_t keep;                  // 0: a row of zeros in the result
     // from the bits of max |x|: not finite -> scale NaN and zeros; scale 0 (or underflown to it) -> zeros
     __device__ __forceinline__ explicit RowScale(uint32_t top) {
         scale = top < 0x7F800000u ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7FC00000u);
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));  // 2^-23 of it off: of 127 steps, 2e-5 of a step
+        keep = scale > 0.f ? 0xFFFFFFFFu : 0u;
+        half = keep ? 0.5f * scale : INFINITY;
+        start = tiny() && keep ? INFINITY : 0.f;
     }
-    __device__ __forceinline__ bool zeros() const { return !(scale > 0.f); }  // NaN too
-    __device__ __forceinline__ bool tiny() const { return scale < 1e-30f; }    // 1 / scale may overflow
-    __device__ __forceinline__ float estimate(float x) const { return fmaf(x, inv, Q_MAGIC); }
-    // what the estimate leaves, at most half of scale where it is right
-    __device__ __forceinline__ float rest(float x, float e) const { return fabsf(fmaf(-(e - Q_MAGIC), scale, x)); }
+    __device__ __forceinline__ bool tiny() const { return scale < 1e-30f; }  // 1 / scale may overflow, scale / 2 may be rounded
     // with care: the neighbour where the remainder passes half a step, the even one where it is half a step
     __device__ __forceinline__ int exact(float x) const {
         float s = scale, i = inv;
@@ -51,8 +51,13 @@ __device__ __forceinline__ uint32_t chunk_top(uint4 v) {
     uint32_t m = 0;
     if constexpr (Chunk<T>::N == 4) {
         m = max(max(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), max(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
-    } else {  // two bf16 to a word, compared as 16-bit integers
-        const uint32_t a = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    } else {  // two bf16 to a word; a NaN wins and becomes 0x7FFF
+        auto larger = [](uint32_t a, uint32_t b) {
+            uint32_t c;
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(a), "r"(b));
+            return c;
+        };
+        const uint32_t a = larger(larger(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), larger(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
         m = max(a << 16, a & 0xFFFF0000u);
     }
     return m;
@@ -61,26 +66,31 @@ template <typename T>
 __device__ __forceinline__ void chunk_out(uint4 v, const RowScale& rs, int8_t* q) {
     constexpr int N = Chunk<T>::N;
     uint32_t w[N / 4];
-    if (rs.zeros()) {
+    float f[N], far = rs.start;
+    uint32_t u[N];
+    Chunk<T>::unpack(v, f);
+    const float2 inv = make_float2(rs.inv, rs.inv), minus = make_float2(-rs.scale, -rs.scale), magic = make_float2(Q_MAGIC, Q_MAGIC);
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) w[k] = 0;
-    } else {
-        float f[N], far = 0.f;
-        uint32_t u[N];
-        Chunk<T>::unpack(v, f);
+    for (int k = 0; k < N; k += 2) {
+        const float2 x = make_float2(f[k], f[k + 1]), e = fma2(x, inv, magic);
+        const float2 r = fma2(add2(e, make_float2(-Q_MAGIC, -Q_MAGIC)), minus, x);
+        u[k] = __float_as_uint(e.x);
+        u[k + 1] = __float_as_uint(e.y);
+        far = fmaxf(fmaxf(far, fabsf(r.x)), fabsf(r.y));
+    }
+    if (far >= rs.half) {  // a value at half a step (of bf16 rows one in 600: half the largest) or one whose estimate fell on the wrong side
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float e = rs.estimate(f[k]);
-            u[k] = __float_as_uint(e);
-            far = fmaxf(far, rs.rest(f[k], e));
+            const float r = fmaf(-(__uint_as_float(u[k]) - Q_MAGIC), rs.scale, f[k]);
+            if (fabsf(r) > rs.half || (fabsf(r) == rs.half && (u[k] & 1u))) u[k] += r > 0.f ? 1 : -1;
         }
-        if (2.f * far >= rs.scale || rs.tiny()) {  // rare
+        if (rs.start > 0.f) {
 #pragma unroll
             for (int k = 0; k < N; ++k) u[k] = (uint32_t)rs.exact(f[k]);
         }
-#pragma unroll
-        for (int k = 0; k < N / 4; ++k) w[k] = __byte_perm(__byte_perm(u[4 * k], u[4 * k + 1], 0x0040), __byte_perm(u[4 * k + 2], u[4 * k + 3], 0x0040), 0x5410);
     }
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) w[k] = __byte_perm(__byte_perm(u[4 * k], u[4 * k + 1], 0x0040), __byte_perm(u[4 * k + 2], u[4 * k + 3], 0x0040), 0x5410) & rs.keep;
     if constexpr (N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(q) = w[0];
 }
@@ -167,7 +177,7 @@ quantize_any_kernel(const T* X, int64_t N, int K, int8_t* __restrict__ q, float*
         __syncthreads();
         const RowScale rs(top);
         if (threadIdx.x == 0) scale[row] = rs.scale;
-        for (int k = threadIdx.x; k < K; k += 256) q[row * K + k] = rs.zeros() ? (int8_t)0 : (int8_t)rs.exact((float)x[k]);
+        for (int k = threadIdx.x; k < K; k += 256) q[row * K + k] = rs.keep ? (int8_t)rs.exact((float)x[k]) : (int8_t)0;
     }
 }
 

@@ -127,18 +127,6 @@ struct LpRun {
     float2 s, t;
     static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
     __device__ __forceinline__ void clear() { m = -INFINITY; r = 0.f; k = LOG2E; s = t = make_float2(0.f, 0.f); }
-    static __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-        float2 d;
-        asm("{.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;}"
-            : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-        return d;
-    }
-    static __device__ __forceinline__ float2 add2(float2 a, float2 b) {
-        float2 d;
-        asm("{.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;}"
-            : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-        return d;
-    }
     static __device__ __forceinline__ float exp2_(float u) {
         float e;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u));
@@ -161,13 +149,14 @@ struct LpRun {
         s = add2(s, e);
         t = fma2(e, make_float2(fmaxf(u.x, -2000.f), fmaxf(u.y, -2000.f)), t);
     }
-    __device__ __forceinline__ LpStats stats() const {
+    // taken_out: of the sums a class at m (the 1 that LpStats leaves out)
+    __device__ __forceinline__ LpStats stats(bool taken_out = false) const {
         LpStats o;
         const float S = s.x + s.y;
         o.m = m;
         if (!(m > -INFINITY) || m == INFINITY) { o.s = S == S && m < INFINITY ? 0.f : __uint_as_float(0x7FC00000u); o.t = 0.f; return o; }
         const float off = fmaf(m, k, -r), f = exp2_(-off);
-        o.s = fmaf(f, S, -1.f);
+        o.s = taken_out ? f * S : fmaf(f, S, -1.f);
         o.t = LN2 * f * fmaf(-off, S, t.x + t.y);
         return o;
     }
@@ -208,41 +197,47 @@ __device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const 
     }
 }
 
-// Few classes, many rows: a thread per row, its scores in registers (CM of them, those past the last one NaN, which no maximum
-// takes).  A block's rows are consecutive in memory: they arrive by whole chunks and are handed over through shared memory, rows
-// an odd number of words apart.  170,000 x 47, five best: by a warp per row 241 us.
+// Few classes, many rows: a thread per row.  A block's rows are consecutive in memory: they arrive by whole chunks and are handed
+// over through shared memory, as they lie (words of a warp's rows then fall on one bank at most two at a time), or, where the
+// number of classes is a multiple of four, in rows of an odd number of 16-byte words.
+// The best: the largest of the groups' largest scores (eight classes each), then its group again in shared memory, where what is
+// taken becomes NaN.  170,000 x 47, five best: by a warp per row 241 us, with a row's scores in registers, looked through for every
+// class listed, 29 us.
 constexpr int LP_ROWS = 128;  // of a block
+constexpr int LP_FEW = 64;    // classes at most: NG groups of eight
+__host__ __device__ constexpr int lp_few_stride(int C) { return C % 4 == 0 ? (C / 4 | 1) * 4 : C; }
 
-template <typename T, int CM>
+template <typename T, int NG>
 __global__ void __launch_bounds__(LP_ROWS)
 log_probs_few_kernel(const LpParams P) {
     pdl_wait();
     constexpr int PER = Chunk<T>::N;
-    extern __shared__ float sh_z[];  // [LP_ROWS][C | 1]
-    const int C = P.C, stride = C | 1;
+    extern __shared__ __align__(16) float sh_z[];  // [LP_ROWS][stride] and a chunk
+    const int C = P.C, stride = lp_few_stride(C);
     const int64_t r0 = (int64_t)blockIdx.x * LP_ROWS;
     const int rows = (int)(P.N - r0 < LP_ROWS ? P.N - r0 : LP_ROWS);
     const T* const z = (const T*)P.z + r0 * C;  // on 16 bytes: LP_ROWS rows are
     const int elements = rows * C;
-    {
-        int r = (int)threadIdx.x * PER / C, c = (int)threadIdx.x * PER - r * C;
-        const int dr = LP_ROWS * PER / C, dc = LP_ROWS * PER - dr * C;
-        for (int e = (int)threadIdx.x * PER; e < elements; e += LP_ROWS * PER) {
+    constexpr int U = 4;  // chunks in flight per thread
+    for (int e0 = (int)threadIdx.x * PER; e0 < elements; e0 += U * LP_ROWS * PER) {
+        uint4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + u * LP_ROWS * PER + PER <= elements) v[u] = ld_16(z + e0 + u * LP_ROWS * PER);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = e0 + u * LP_ROWS * PER;
             float f[PER];
-            if (e + PER <= elements) Chunk<T>::unpack(ld_16(z + e), f);
+            if (e >= elements) break;
+            if (e + PER <= elements) Chunk<T>::unpack(v[u], f);
             else
 #pragma unroll
                 for (int k = 0; k < PER; ++k) f[k] = e + k < elements ? (float)z[e + k] : 0.f;
-            int at = r * stride + c, left = C - c;  // to the end of the row
 #pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                if (e + k < elements) sh_z[at] = f[k];
-                ++at;
-                if (--left == 0) { left = C; at += stride - C; }
+            for (int k = 0; k < PER; k += 4) {  // (four lie in one row where rows are padded)
+                const int at = stride == C ? e + k : e + k + (int)((unsigned)(e + k) / (unsigned)C) * (stride - C);
+                *reinterpret_cast<float4*>(sh_z + at) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
             }
-            r += dr;
-            c += dc;
-            if (c >= C) { c -= C; ++r; }
         }
     }
     __syncthreads();
@@ -250,34 +245,54 @@ log_probs_few_kernel(const LpParams P) {
     const int64_t row = r0 + threadIdx.x;
     float* const mine = sh_z + threadIdx.x * stride;
     const float nan = __uint_as_float(0x7FC00000u);
-    float v[CM];
+    // groups of eight classes, the last may be cut: their largest
+    const int full = C / 8;
+    float gm[NG];
+    float m = nan;
 #pragma unroll
-    for (int c = 0; c < CM; ++c) v[c] = c < C ? mine[c] : nan;
-    auto largest = [&]() {
-        float m = v[0];
+    for (int g = 0; g < NG; ++g) {
+        gm[g] = nan;
+        if (g < full) {
 #pragma unroll
-        for (int c = 1; c < CM; ++c) m = fmaxf(m, v[c]);
-        return m;
-    };
-    // the first class at m
-    auto where = [&](float m) {
-        int at = CM;
+            for (int c = 0; c < 8; ++c) gm[g] = fmaxf(gm[g], mine[8 * g + c]);
+        } else if (g == full) {
+            for (int c = 8 * g; c < C; ++c) gm[g] = fmaxf(gm[g], mine[c]);
+        }
+        m = fmaxf(m, gm[g]);
+    }
+    // the first class at m (C: there is no number left); its group's next largest takes its place
+    auto take = [&](float m) {
+        int first = NG;
 #pragma unroll
-        for (int c = CM - 1; c >= 0; --c) at = v[c] == m ? c : at;
+        for (int g = NG - 1; g >= 0; --g) first = gm[g] == m ? g : first;
+        if (first == NG) return C;
+        int at = C;
+        float next = nan;
+#pragma unroll
+        for (int c = 7; c >= 0; --c) {
+            const float x = 8 * first + c < C ? mine[8 * first + c] : nan;
+            const bool hit = x == m;
+            next = hit ? (at < C ? m : next) : fmaxf(next, x);  // an equal one stays
+            at = hit ? 8 * first + c : at;
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) gm[g] = g == first ? next : gm[g];
         return at;
     };
-    LpStats st;
-    st.clear();
-    st.m = largest();
-    const int lead = where(st.m);
-    const bool nothing = !(st.m > -INFINITY);  // -inf, or NaN throughout
-    if (nothing) st.m = -INFINITY;
-    const float base = nothing ? 0.f : st.m;
-#pragma unroll
-    for (int c = 0; c < CM; ++c) {
-        if (c >= C) break;
-        if (c != lead || nothing) st.add(v[c], base);
+    const int lead = take(m);
+    // the sums without the leading class: at -inf meanwhile
+    LpRun run;
+    run.clear();
+    if (m > -INFINITY) {
+        run.raise(m);
+        mine[lead] = -INFINITY;
     }
+    for (int g = 0; g < full; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) run.add(mine[8 * g + c], mine[8 * g + c + 1]);
+    for (int c = 8 * full; c < C; ++c) run.add(mine[c], -INFINITY);
+    if (lead < C) mine[lead] = nan;  // taken
+    const LpStats st = run.stats(true);
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
     const float tail = log1pf(st.s);
     auto logp = [&](float x) { return bad ? nan : none || x == -INFINITY ? -INFINITY : (x - st.m) - tail; };
@@ -285,45 +300,23 @@ log_probs_few_kernel(const LpParams P) {
     if (P.entropy) P.entropy[row] = bad ? nan : none ? 0.f : tail - st.t / (1.f + st.s);
     if (P.logp) {
         const int y = P.label[row];
-        P.logp[row] = y >= 0 && y < C ? logp(mine[y]) : 0.f;
-    }
-    // The best: the largest of the groups' largest scores (eight classes each), then its group again in shared memory, where what is
-    // taken becomes NaN.  (All CM scores in registers looked through for every class listed: 29 us instead of XX.)
-    float gm[CM / 8];
-#pragma unroll
-    for (int g = 0; g < CM / 8; ++g) {
-        gm[g] = v[8 * g];
-#pragma unroll
-        for (int c = 1; c < 8; ++c) gm[g] = fmaxf(gm[g], v[8 * g + c]);
+        P.logp[row] = y >= 0 && y < C ? logp(y == lead ? m : mine[y]) : 0.f;
     }
     for (int j = 0; j < P.top; ++j) {
-        float m = gm[0];
+        int at = lead;
+        if (j > 0) {
+            m = gm[0];
 #pragma unroll
-        for (int g = 1; g < CM / 8; ++g) m = fmaxf(m, gm[g]);
-        int first = CM / 8;
-#pragma unroll
-        for (int g = CM / 8 - 1; g >= 0; --g) first = gm[g] == m ? g : first;
-        int at = C;
-        if (first < CM / 8) {
-            float next = nan;
-#pragma unroll
-            for (int c = 7; c >= 0; --c) {
-                const float x = 8 * first + c < C ? mine[8 * first + c] : nan;
-                if (x == m) {
-                    next = at < C ? m : next;  // the one after it stays, an equal
-                    at = 8 * first + c;
-                } else {
-                    next = fmaxf(next, x);
-                }
-            }
-            mine[at] = nan;
-#pragma unroll
-            for (int g = 0; g < CM / 8; ++g) gm[g] = g == first ? next : gm[g];
-        } else {  // numbers are used up: what is not one, in order
+            for (int g = 1; g < NG; ++g) m = fmaxf(m, gm[g]);
+            at = take(m);
+            if (at < C) mine[at] = nan;
+        }
+        if (at == C) {  // numbers are used up: what is not one, in order
+            const T* const orig = z + (int64_t)threadIdx.x * C;
             int skip = j;
-            for (int c = 0; c < C; ++c) skip -= !((float)z[threadIdx.x * C + c] != (float)z[threadIdx.x * C + c]);
+            for (int c = 0; c < C; ++c) skip -= (float)orig[c] == (float)orig[c];
             for (int c = 0; c < C; ++c)
-                if ((float)z[threadIdx.x * C + c] != (float)z[threadIdx.x * C + c] && skip-- == 0) at = c;
+                if ((float)orig[c] != (float)orig[c] && skip-- == 0) at = c;
             m = nan;
         }
         P.top_idx[row * P.top + j] = at;
@@ -331,16 +324,32 @@ log_probs_few_kernel(const LpParams P) {
     }
 }
 
-// the statistics of a warp's lanes, in the same order for both sides of a pair
+// The statistics of a warp's lanes joined, all lanes alike: every lane's sum scaled to the largest maximum, that of the first lane
+// that has it without its own 1.
 __device__ __forceinline__ void lp_join_lanes(LpStats& st, int lane) {
+    float m = st.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const bool lead = lane == __ffs(__ballot_sync(0xFFFFFFFFu, st.m == m)) - 1;  // m is a number or -inf: some lane has it
+    const float d = st.m - m, f = lp_exp(d), c = f * (st.s + 1.f);  // a lane without classes: -inf - m (NaN where m is -inf as well: below)
+    float s = st.m == -INFINITY ? 0.f * st.s : lead ? st.s : c;
+    float t = st.m == -INFINITY ? 0.f : lead ? st.t : fmaf(fmaxf(d, -1000.f), c, f * st.t);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        LpStats q;
-        q.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, o);
-        q.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, o);
-        q.t = __shfl_xor_sync(0xFFFFFFFFu, st.t, o);
-        if (lane & o) { LpStats a = q; a.join(st); st = a; } else st.join(q);
+        s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
     }
+    st.m = m;
+    st.s = s;
+    st.t = t;
+}
+// ... and of the block's eight warps, joined by every warp
+__device__ __forceinline__ LpStats lp_join_warps(const LpStats* sh, int lane) {
+    LpStats st;
+    st.clear();
+    if (lane < 8) st = sh[lane];
+    lp_join_lanes(st, lane);
+    return st;
 }
 
 // Rows by W warps (1: eight rows a block; 8: a row, or a part of one, per block), in one pass over the scores.
@@ -368,7 +377,7 @@ log_probs_kernel(const LpParams P) {
     const int part = W == 1 ? 0 : (int)(blockIdx.x % P.parts);
     if (row >= P.N) return;  // (W = 1: a whole warp; no block-wide step follows)
     const T* const z = (const T*)P.z;
-    // 16-byte chunks of the whole matrix that hold elements of the row: the first and the last may hold others' too
+    // 16-byte chunks of the whole matrix that hold elements of the row (of the part): the row's first and last may hold others' too
     const int64_t e0 = row * P.C, e1 = e0 + P.C, all = P.N * P.C;
     int64_t c0 = e0 / PER, c1 = (e1 + PER - 1) / PER;
     if (P.parts > 1) {
@@ -376,40 +385,43 @@ log_probs_kernel(const LpParams P) {
         c1 = n1 < c1 ? n1 : c1;
         c0 = n0;
     }
+    const int count = c1 > c0 ? (int)(c1 - c0) : 0;
+    const T* const zc = z + c0 * PER;
+    const int first_class = (int)(c0 * PER - e0);             // class of the first element of chunk 0; negative: another row's
+    const int whole = (int)((all - c0 * PER) / PER < count ? (all - c0 * PER) / PER : count);  // chunks that end inside the matrix
     const int me = W == 1 ? lane : threadIdx.x;
     constexpr int STEP = W * 32;
-    // chunk i of the matrix; elements outside the row: -inf, and not `in`
-    auto load = [&](int64_t i) {
-        if ((i + 1) * PER <= all) return ld_16(z + i * PER);
+    auto load = [&](int i) {
+        if (i < whole) return ld_16(zc + (int64_t)i * PER);
         union { T e[PER]; uint4 q; } x;
 #pragma unroll
-        for (int k = 0; k < PER; ++k) x.e[k] = i * PER + k < all ? z[i * PER + k] : T(0.f);
+        for (int k = 0; k < PER; ++k) x.e[k] = c0 * PER + (int64_t)i * PER + k < all ? zc[(int64_t)i * PER + k] : T(0.f);
         return x.q;
     };
-    auto inside = [&](int64_t i, int k) { return i * PER + k >= e0 && i * PER + k < e1; };
+    auto inside = [&](int i, int k) { return (unsigned)(first_class + i * PER + k) < (unsigned)P.C; };
+    auto scores = [&](int i, uint4 v, float* f) {  // those of other rows: -inf
+        Chunk<T>::unpack(v, f);
+        if (!inside(i, 0) || !inside(i, PER - 1)) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (!inside(i, k)) f[k] = -INFINITY;
+        }
+    };
     LpRun run;
     run.clear();
     const bool list = P.top > 0;
     constexpr int U = 4;  // chunks in flight per lane
     int n = 0;
-    for (int64_t c = c0; c < c1; c += U * STEP) {  // the same for all lanes
+    for (int c = me; c - me < count; c += U * STEP) {  // the same for all lanes
         uint4 v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t i = c + u * STEP + me;
-            if (i < c1) v[u] = load(i);
-        }
+        for (int u = 0; u < U; ++u)
+            if (c + u * STEP < count) v[u] = load(c + u * STEP);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t i = c + u * STEP + me;
-            if (i >= c1) break;
+            if (c + u * STEP >= count) break;
             float f[PER];
-            Chunk<T>::unpack(v[u], f);
-            if (i * PER < e0 || (i + 1) * PER > e1) {
-#pragma unroll
-                for (int k = 0; k < PER; ++k)
-                    if (!inside(i, k)) f[k] = -INFINITY;
-            }
+            scores(c + u * STEP, v[u], f);
             float cm = f[0];
 #pragma unroll
             for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
@@ -428,12 +440,11 @@ log_probs_kernel(const LpParams P) {
     if constexpr (W > 1) {
         if (lane == 0) sh_stats[warp] = st;
         __syncthreads();
-        st = sh_stats[0];
-        for (int w = 1; w < W; ++w) st.join(sh_stats[w]);  // all warps alike
+        st = lp_join_warps(sh_stats, lane);
     }
     // One class takes most of it: the sum beside its own 1 has lost digits in the thread that holds it.  That thread's chunks again,
     // without the 1, by its warp; the other threads' sums stand.
-    if (st.s < 2.f && st.m > -INFINITY && st.m < INFINITY) {
+    if (st.s < 0.0625f && st.m > -INFINITY && st.m < INFINITY) {
         const uint32_t at = __ballot_sync(0xFFFFFFFFu, mine == st.m);
         int owner = at ? warp * 32 + __ffs(at) - 1 : 256;
         if constexpr (W > 1) {
@@ -450,22 +461,19 @@ log_probs_kernel(const LpParams P) {
             again.clear();
             again.m = st.m;
             bool taken = false;  // the first of its classes at the maximum
-            for (int64_t c = c0 + who; c < c1; c += 32 * STEP) {
-                const int64_t i = c + (int64_t)lane * STEP;
+            for (int c = who; c < count; c += 32 * STEP) {
+                const int i = c + lane * STEP;
                 float f[PER];
                 bool hit = false;
-                if (i < c1) {
-                    Chunk<T>::unpack(load(i), f);
+                if (i < count) {
+                    scores(i, load(i), f);
 #pragma unroll
-                    for (int k = 0; k < PER; ++k) {
-                        if (!inside(i, k)) f[k] = -INFINITY;
-                        hit |= f[k] == st.m;
-                    }
+                    for (int k = 0; k < PER; ++k) hit |= f[k] == st.m;
                 }
                 const uint32_t hits = __ballot_sync(0xFFFFFFFFu, hit);
                 bool skip = !taken && hits && lane == __ffs(hits) - 1;
                 taken |= hits != 0;
-                if (i < c1) {
+                if (i < count) {
 #pragma unroll
                     for (int k = 0; k < PER; ++k) {
                         if (skip && f[k] == st.m) skip = false;
@@ -485,8 +493,7 @@ log_probs_kernel(const LpParams P) {
         if constexpr (W > 1) {
             if (lane == 0) sh_stats[warp] = st;
             __syncthreads();
-            st = sh_stats[0];
-            for (int w = 1; w < W; ++w) st.join(sh_stats[w]);
+            st = lp_join_warps(sh_stats, lane);
         }
     }
     uint64_t best = 0;
@@ -509,29 +516,29 @@ log_probs_kernel(const LpParams P) {
         }
         for (int k = 0; k < n; ++k) {
             if (!(sh_max[k * 256 + threadIdx.x] >= floor)) continue;
-            const int64_t i = c0 + (int64_t)k * STEP + me;
+            const int i = k * STEP + me;
             float f[PER];
             Chunk<T>::unpack(load(i), f);
 #pragma unroll
             for (int e = 0; e < PER; ++e)
                 if (f[e] >= floor && inside(i, e)) {
                     const int at = atomicAdd(&sh_count[g], 1);
-                    if (at < LP_CAND) sh_cand[g][at] = lp_key(f[e], (uint32_t)(i * PER + e - e0));
+                    if (at < LP_CAND) sh_cand[g][at] = lp_key(f[e], (uint32_t)(first_class + i * PER + e));
                 }
         }
         if constexpr (W == 1) __syncwarp(); else __syncthreads();
-        const int count = sh_count[g];
-        if (count >= P.top && count <= LP_CAND) {
-            if (W == 1 || warp == 0) best = lp_best_of(sh_cand[g], count, lane);
+        const int found = sh_count[g];
+        if (found >= P.top && found <= LP_CAND) {
+            if (W == 1 || warp == 0) best = lp_best_of(sh_cand[g], found, lane);
         } else {
             LpTop one;
             one.clear();
-            for (int64_t c = c0; c < c1; c += STEP) {
-                const int64_t i = c + me;
+            for (int c = 0; c < count; c += STEP) {
+                const int i = c + me;
                 float f[PER];
-                if (i < c1) Chunk<T>::unpack(load(i), f);
+                if (i < count) Chunk<T>::unpack(load(i), f);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) one.offer(i < c1 && inside(i, e) ? lp_key(f[e], (uint32_t)(i * PER + e - e0)) : 0, P.top, lane);
+                for (int e = 0; e < PER; ++e) one.offer(i < count && inside(i, e) ? lp_key(f[e], (uint32_t)(first_class + i * PER + e)) : 0, P.top, lane);
             }
             best = one.key;
             if constexpr (W > 1) {
@@ -609,7 +616,7 @@ log_probs_join_kernel(const LpParams P) {
         __syncthreads();
     }
     if (warp != 0) return;
-    for (int w = 1; w < 8; ++w) st.join(sh_stats[w]);
+    st = lp_join_warps(sh_stats, lane);
     lp_finish<T>(P, row, st, P.top > 0 ? lp_best_of(sh_cand, sh_count, lane) : 0, lane);
 }
 
@@ -723,18 +730,22 @@ log_probs_backward_kernel(const LpGradParams P) {
     }
 }
 
-// Blocks per row: as many as give the SMs twelve blocks each while every block has 8 KB of the row at least; and enough that a
-// thread has LP_CHUNKS chunks at most.
+// Blocks per row: what makes the fewest rounds of four blocks per SM times the chunks per thread of a block, to which its fixed part
+// (joining, sorting) adds about 14; a block has 8 KB of the row at least, a thread LP_CHUNKS chunks at most.
 static int64_t lp_parts(int64_t N, int64_t C, int s) {
     const int64_t bytes = C * s, least = ceil_div(bytes + 16, (int64_t)LP_CHUNKS * 256 * 16 - 16);
-    int64_t p = N < 148 * 4 ? (148 * 12) / N : 1;
-    const int64_t most = bytes / (8 * 1024);
-    p = p < most ? p : most;
-    return p > least ? p : least;
+    int64_t most = bytes / (8 * 1024);
+    if (most > 592) most = 592;
+    if (N >= 592 * 8 || most <= least) return least;
+    auto cost = [&](int64_t p) { return (double)ceil_div(N * p, 592) * ((double)bytes / 4096 / (double)p + 14.0); };
+    int64_t best = least;
+    for (int64_t p = least + 1; p <= most; ++p)
+        if (cost(p) < 0.98 * cost(best)) best = p;
+    return best;
 }
 
 // a thread per row: few classes, and rows enough to fill the SMs with threads
-static bool lp_few(int64_t N, int C, int top) { return C <= 64 && N >= 4096; }
+static bool lp_few(int64_t N, int C, int top) { return C <= LP_FEW && N >= 4096; }
 
 struct LpWs {
     int64_t parts;
@@ -779,12 +790,10 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
     const int64_t chunks = (int64_t)C / (f32 ? 4 : 8) + 2;  // of a row, both ends cut
     if (lp_few(N, C, top)) {
         const dim3 grid((unsigned)ceil_div(N, LP_ROWS));
-        const size_t smem = (size_t)LP_ROWS * (C | 1) * 4;
+        const size_t smem = ((size_t)LP_ROWS * lp_few_stride(C) + 8) * 4;
         auto run = [&](auto kernel) { launch_overlapped(kernel, grid, dim3(LP_ROWS), smem, st, P); };
-        if (f32) C <= 8 ? run(log_probs_few_kernel<float, 8>) : C <= 16 ? run(log_probs_few_kernel<float, 16>) : C <= 32 ? run(log_probs_few_kernel<float, 32>)
-               : C <= 48 ? run(log_probs_few_kernel<float, 48>) : run(log_probs_few_kernel<float, 64>);
-        else C <= 8 ? run(log_probs_few_kernel<__nv_bfloat16, 8>) : C <= 16 ? run(log_probs_few_kernel<__nv_bfloat16, 16>) : C <= 32 ? run(log_probs_few_kernel<__nv_bfloat16, 32>)
-           : C <= 48 ? run(log_probs_few_kernel<__nv_bfloat16, 48>) : run(log_probs_few_kernel<__nv_bfloat16, 64>);
+        if (f32) C <= 16 ? run(log_probs_few_kernel<float, 2>) : C <= 32 ? run(log_probs_few_kernel<float, 4>) : C <= 48 ? run(log_probs_few_kernel<float, 6>) : run(log_probs_few_kernel<float, 8>);
+        else C <= 16 ? run(log_probs_few_kernel<__nv_bfloat16, 2>) : C <= 32 ? run(log_probs_few_kernel<__nv_bfloat16, 4>) : C <= 48 ? run(log_probs_few_kernel<__nv_bfloat16, 6>) : run(log_probs_few_kernel<__nv_bfloat16, 8>);
     } else if (C <= LP_WARP_CLASSES) {
         const dim3 grid((unsigned)ceil_div(N, 8));
         const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32) * 1024 : 0;
