@@ -187,9 +187,10 @@ static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scal
     const int chunks = K / PER;
     auto run = [&](auto kernel, int lanes) { launch_overlapped(kernel, dim3((unsigned)ceil_div(N * lanes, 256)), dim3(256), 0, st, X, N, K, q, scale); };
     const dim3 rows((unsigned)(N < 148 * 8 ? N : 148 * 8));
-    if (K % PER == 0 && chunks > 256 && chunks <= 2048) {
+    // (a block per row from 512 chunks on: below, 16,384 x 2048 fp32, a block per row takes 41 us)
+    if (K % PER == 0 && chunks > 512 && chunks <= 2048) {
         auto run_long = [&](auto kernel) { launch_overlapped(kernel, rows, dim3(256), 0, st, X, N, K, q, scale); };
-        chunks <= 512 ? run_long(quantize_long_rows_kernel<T, 2>) : chunks <= 1024 ? run_long(quantize_long_rows_kernel<T, 4>) : run_long(quantize_long_rows_kernel<T, 8>);
+        chunks <= 1024 ? run_long(quantize_long_rows_kernel<T, 4>) : run_long(quantize_long_rows_kernel<T, 8>);
         return;
     }
     if (K % PER != 0 || chunks > 2048) {
@@ -204,7 +205,8 @@ static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scal
     else if (chunks <= 32) run(quantize_rows_kernel<T, 8, 4>, 8);
     else if (chunks <= 64) run(quantize_rows_kernel<T, 16, 4>, 16);
     else if (chunks <= 128) run(quantize_rows_kernel<T, 32, 4>, 32);
-    else run(quantize_rows_kernel<T, 32, 8>, 32);
+    else if (chunks <= 256) run(quantize_rows_kernel<T, 32, 8>, 32);
+    else run(quantize_rows_kernel<T, 32, 16>, 32);
 }
 
 // ------------------------------------------------------------------ the product

@@ -123,10 +123,15 @@ __device__ __forceinline__ uint64_t lp_best_of(const uint64_t* keys, int n, int 
 // by is taken out at the end.  Beyond |m| = 1e37, where m log2(e) could overflow, neighbouring numbers are 1e30 apart: 2^(z / 4 - m / 4)
 // tells as well who is at m, and all others are 0.
 struct LpRun {
-    float m, r, k;
+    float m, r;
+    float2 k, minus;  // the factor, and -r, twice each
     float2 s, t;
     static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-    __device__ __forceinline__ void clear() { m = -INFINITY; r = 0.f; k = LOG2E; s = t = make_float2(0.f, 0.f); }
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY; r = 0.f;
+        k = make_float2(LOG2E, LOG2E);
+        minus = s = t = make_float2(0.f, 0.f);
+    }
     static __device__ __forceinline__ float exp2_(float u) {
         float e;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u));
@@ -135,16 +140,17 @@ struct LpRun {
     // the maximum becomes v > m
     __device__ __forceinline__ void raise(float v) {
         const bool first = m == -INFINITY;
-        k = fabsf(v) > 1e37f ? 0.25f : LOG2E;
-        const float q = v * k, d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
+        k.x = k.y = fabsf(v) > 1e37f ? 0.25f : LOG2E;
+        const float q = v * k.x, d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
         t = first ? make_float2(0.f, 0.f) : make_float2(f * fmaf(d, s.x, t.x), f * fmaf(d, s.y, t.y));
         s = make_float2(f * s.x, f * s.y);  // (not a number stays one)
         m = v;
         r = q;
+        minus = make_float2(-q, -q);
     }
     // two scores, neither above m; -inf: 2^-inf = 0 times a finite exponent
     __device__ __forceinline__ void add(float a, float b) {
-        const float2 u = fma2(make_float2(a, b), make_float2(k, k), make_float2(-r, -r));
+        const float2 u = fma2(make_float2(a, b), k, minus);
         const float2 e = make_float2(exp2_(u.x), exp2_(u.y));
         s = add2(s, e);
         t = fma2(e, make_float2(fmaxf(u.x, -2000.f), fmaxf(u.y, -2000.f)), t);
@@ -155,7 +161,7 @@ struct LpRun {
         const float S = s.x + s.y;
         o.m = m;
         if (!(m > -INFINITY) || m == INFINITY) { o.s = S == S && m < INFINITY ? 0.f : __uint_as_float(0x7FC00000u); o.t = 0.f; return o; }
-        const float off = fmaf(m, k, -r), f = exp2_(-off);
+        const float off = fmaf(m, k.x, -r), f = exp2_(-off);
         o.s = taken_out ? f * S : fmaf(f, S, -1.f);
         o.t = LN2 * f * fmaf(-off, S, t.x + t.y);
         return o;
@@ -352,6 +358,22 @@ __device__ __forceinline__ LpStats lp_join_warps(const LpStats* sh, int lane) {
     return st;
 }
 
+// largest of a chunk, what is not a number left out (NaN where there is none)
+template <typename T>
+__device__ __forceinline__ float lp_chunk_max(uint4 v) {
+    if constexpr (Chunk<T>::N == 4) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    } else {
+        auto larger = [](uint32_t a, uint32_t b) {
+            uint32_t c;
+            asm("max.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(a), "r"(b));
+            return c;
+        };
+        const uint32_t m = larger(larger(v.x, v.y), larger(v.z, v.w));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    }
+}
+
 // Rows by W warps (1: eight rows a block; 8: a row, or a part of one, per block), in one pass over the scores.
 // The best classes: every thread keeps the largest score of each of its chunks (shared memory).  The k-th largest of the
 // threads' own largest scores is a floor of the k-th best class; only chunks that reach it are looked at again (in L1 or L2),
@@ -412,8 +434,31 @@ log_probs_kernel(const LpParams P) {
     const bool list = P.top > 0;
     constexpr int U = 4;  // chunks in flight per lane
     int n = 0;
+    // chunks of the row alone: all but its two ends
+    const int lo = first_class < 0 ? 1 : 0, hi = (int64_t)first_class + (int64_t)count * PER > P.C ? count - 1 : count;
     for (int c = me; c - me < count; c += U * STEP) {  // the same for all lanes
         uint4 v[U];
+        if (c >= lo && c + (U - 1) * STEP < hi) {  // four whole chunks: the maximum rises once at most
+            float cm[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = ld_16(zc + (int64_t)(c + u * STEP) * PER);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                cm[u] = lp_chunk_max<T>(v[u]);
+                if (list) sh_max[(n + u) * 256 + threadIdx.x] = cm[u];
+            }
+            const float bm = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
+            n += U;
+            if (bm > run.m) run.raise(bm);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[PER];
+                Chunk<T>::unpack(v[u], f);
+#pragma unroll
+                for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+            }
+            continue;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (c + u * STEP < count) v[u] = load(c + u * STEP);
@@ -425,10 +470,8 @@ log_probs_kernel(const LpParams P) {
             float cm = f[0];
 #pragma unroll
             for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
-            if (list) {
-                sh_max[n * 256 + threadIdx.x] = cm;
-                ++n;
-            }
+            if (list) sh_max[n * 256 + threadIdx.x] = cm;
+            ++n;
             if (cm > run.m) run.raise(cm);
 #pragma unroll
             for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
