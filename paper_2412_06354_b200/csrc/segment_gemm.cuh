@@ -24,8 +24,9 @@
 //   warp 1     issues the tcgen05.mma of a slice into one of two accumulators in tensor memory.  SG_DW: the rows of a segment's
 //              last slice that belong to the next one are overwritten with zeros first, in both operands (a zero in one would
 //              not do: they may hold infinities)
-//   warps 2-9  epilogue: accumulator -> registers -> swizzled staging -> whole rows to global memory, rows and columns that do
-//              not exist left out
+//   warps 2-17 epilogue: accumulator -> registers -> swizzled staging -> rows of 64 bytes to global memory, rows and columns that
+//              do not exist left out.  (Eight warps with 128 bytes: 8-bit product of 170,000 x 256 -> 256 40 us, of which 20 without
+//              any epilogue.)
 // fp32 (segment_gemm_f32_kernel): the same pieces of work, every value as three bf16 terms.
 //
 // Every wait has an iteration limit, as in linear_tma.cu.
@@ -40,12 +41,12 @@ namespace gnn {
 
 enum { SG_Y = 0, SG_DX = 1, SG_DW = 2, SG_I8 = 3 };
 
-constexpr int SG_EPI_WARPS = 8;
+constexpr int SG_EPI_WARPS = 16;
 constexpr int SG_THREADS = 32 * (2 + SG_EPI_WARPS);
 constexpr int SG_MAX_STAGES = 8;
 constexpr size_t SG_SMEM_MAX = 224 * 1024;      // dynamic; with the static part on its 1024-byte boundary: the 227 KB of a block
 constexpr uint32_t SG_A_BYTES = 128 * 128;      // 128 rows of 128 bytes (SG_DW: two boxes of 64 features x 64 rows)
-constexpr uint32_t SG_STAGING = 32 * 128;       // per epilogue warp
+constexpr uint32_t SG_STAGING = 32 * 64;        // per epilogue warp: 32 rows of 64 bytes
 constexpr uint32_t SG_SW128 = 2;
 
 struct SegGemmParams {
@@ -72,56 +73,90 @@ struct SegGemmParams {
 };
 
 // rows [lo, hi) of segment g, kept inside [0, N) whatever seg_ptr holds
-struct SegRows { int64_t lo, hi; int g; };
+struct SegRows { int64_t lo, hi; int g; int64_t a, b; };  // a, b: all rows of the segment
 __device__ __forceinline__ int64_t seg_at(const SegGemmParams& P, int g) {
     if (!P.seg_ptr) return g > 0 ? P.N : 0;
     const int64_t v = P.seg_ptr[g];
     return v < 0 ? 0 : v > P.N ? P.N : v;
 }
-// last g in [0, G) with before(g) true for it (before is true up to some g); -1: none.  All lanes of a warp.
+// Last g in [0, G) with before(g, seg_ptr[g]) true for it (before is true up to some g), and its rows; g = -1: none.  All lanes of a
+// warp; the last step has the bounds at hand, so that up to 31 segments take one round of loads.
+struct SegFound { int g; int64_t a, b; };
 template <class F>
-__device__ __forceinline__ int last_segment(int G, F before) {
-    int lo = 0, hi = G;
+__device__ __forceinline__ SegFound last_segment(const SegGemmParams& P, F before) {
+    int lo = 0, hi = P.G;
     const int lane = threadIdx.x & 31;
     while (true) {
         const int step = (hi - lo + 31) >> 5;
         const int p = lo + lane * step;
-        const int n = __popc(__ballot_sync(0xFFFFFFFFu, p < hi && before(p)));
-        if (n == 0) return lo - 1;
+        const int64_t v = p <= P.G ? seg_at(P, p) : P.N;
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, p < hi && before(p, v)));
+        if (n == 0) return {lo - 1, 0, 0};
+        if (step == 1) {
+            const int g = lo + n - 1;
+            const int64_t a = __shfl_sync(0xFFFFFFFFu, v, n - 1), b = __shfl_sync(0xFFFFFFFFu, v, n & 31);
+            return {g, a, n < 32 ? b : seg_at(P, g + 1)};
+        }
         lo += (n - 1) * step;
-        if (step == 1) return lo;
         hi = min(hi, lo + step);
     }
 }
-// tile number s -> its rows (hi <= lo: none)
-__device__ __forceinline__ SegRows seg_tile(const SegGemmParams& P, int64_t s) {
-    const int g = last_segment(P.G, [&](int q) { return seg_at(P, q) / TC_ROWS + q <= s; });
-    if (g < 0) return {0, 0, 0};
-    const int64_t a = seg_at(P, g), b = seg_at(P, g + 1);
-    const int64_t lo = a + (s - (a / TC_ROWS + g)) * TC_ROWS;
-    return {lo, lo + TC_ROWS < b ? lo + TC_ROWS : b, g};
-}
+// Tile number s -> its rows (hi <= lo: none), for ascending s: the segment of the last tile is kept, so that most tiles are two
+// comparisons and an addition.  (Searching anew for each, with 64-bit divisions, the loader took 3400 cycles a tile and was the bound
+// of 170,000 x 128 -> 128.)
+struct SegCursor {
+    int g;
+    int64_t a, b, first, next;  // rows of segment g, its tile numbers
+    __device__ __forceinline__ SegCursor() : g(0), a(0), b(0), first(0), next(0) {}
+    __device__ __forceinline__ SegRows tile(const SegGemmParams& P, int64_t s) {
+        if (s >= next) {
+            const SegFound f = last_segment(P, [&](int q, int64_t v) { return (v >> 7) + q <= s; });
+            if (f.g < 0) return {0, 0, 0, 0, 0};
+            g = f.g;
+            a = f.a;
+            b = f.b;
+            first = (a >> 7) + g;
+            next = (b >> 7) + g + 1;  // (of the next segment; not above the true bound where seg_ptr descends)
+        }
+        const int64_t lo = a + ((s - first) << 7);
+        return {lo, lo + TC_ROWS < b ? lo + TC_ROWS : b, g, a, b};
+    }
+};
 
+// a bounded wait of a whole warp, with one answer
+__device__ __forceinline__ bool sg_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity)); }
+// What one thread of a warp does, called by the whole warp: the election stands in the instruction itself, so that the control flow
+// around it stays that of a whole warp.  (As a branch of lane 0 around loops of them, copies took 250 cycles each to issue and MMAs
+// 85.)  The same thread is elected every time.
+#define SG_ELECT "{\n\t.reg .pred p, q;\n\telect.sync _|p, 0xFFFFFFFF;\n\t"
 __device__ __forceinline__ void sg_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
-        : "memory");
+    asm volatile(SG_ELECT
+                 "@p cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;\n\t}"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void sg_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile(SG_ELECT "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void sg_commit(uint32_t bar) {
+    asm volatile(SG_ELECT "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
+// D (+)= A B: A in shared memory (a descriptor) or in tensor memory (an address)
+__device__ __forceinline__ void sg_mma_bf16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(SG_ELECT "setp.ne.b32 q, %4, 0;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, q;\n\t}"
+                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void sg_mma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(SG_ELECT "setp.ne.b32 q, %4, 0;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, q;\n\t}"
+                 ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void sg_mma_i8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(SG_ELECT "setp.ne.b32 q, %4, 0;\n\t@p tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, q;\n\t}"
+                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 // 8-bit integers: D = s32, A = B = s8, both K-major, 32 contraction elements
 __host__ __device__ constexpr uint32_t make_idesc_i8(int n) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(TC_ROWS >> 4) << 24);
-}
-__device__ __forceinline__ void mma_i8_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t"
-        "}\n"
-        :
-        : "r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
-        : "memory");
 }
 __device__ __forceinline__ uint64_t policy_normal() {
     uint64_t p;
@@ -132,19 +167,31 @@ __device__ __forceinline__ uint64_t policy_normal() {
 // it says stop.
 template <int MODE, class Body>
 __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
-    for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
-        const int n = (int)(u % P.tiles_n);
-        if constexpr (MODE != SG_DW) {
-            const SegRows t = seg_tile(P, u / P.tiles_n);
-            if (t.hi > t.lo && !body(t, 0, n, (int64_t)0)) return;
-        } else {
+    if constexpr (MODE != SG_DW) {
+        // unit = tile number * tiles_n + block of columns
+        const unsigned nn = (unsigned)P.tiles_n, ds = gridDim.x / nn, dn = gridDim.x % nn;
+        unsigned n = blockIdx.x % nn;
+        int64_t s = blockIdx.x / nn;
+        SegCursor at;
+        for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
+            const SegRows t = at.tile(P, s);
+            if (t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            s += ds;
+            n += dn;
+            if (n >= nn) { n -= nn; ++s; }
+        }
+    } else {
+        for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
+            const int n = (int)(u % P.tiles_n);
             const int64_t v = u / P.tiles_n, part = v / P.tiles_m;
             const int64_t r0 = part * P.part_rows, r1 = r0 + P.part_rows < P.N ? r0 + P.part_rows : P.N;
-            int g = last_segment(P.G, [&](int q) { return seg_at(P, q) <= r0; });
-            for (g = g < 0 ? 0 : g; g < P.G; ++g) {
-                const int64_t a = seg_at(P, g), b = seg_at(P, g + 1);
+            SegFound f = last_segment(P, [&](int, int64_t v) { return v <= r0; });
+            int g = f.g;
+            int64_t a = f.a, b = f.b;
+            if (g < 0) { g = 0; a = seg_at(P, 0); b = seg_at(P, 1); }
+            for (; g < P.G; ++g, a = b, b = g < P.G ? seg_at(P, g + 1) : b) {
                 if (a >= r1) break;
-                const SegRows t = {a > r0 ? a : r0, b < r1 ? b : r1, g};
+                const SegRows t = {a > r0 ? a : r0, b < r1 ? b : r1, g, a, b};
                 if (t.hi > t.lo && !body(t, (int)(v % P.tiles_m), n, part)) return;
             }
         }
@@ -154,52 +201,56 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
 __device__ __forceinline__ void sg_store(float* p, uint32_t bits) { *reinterpret_cast<uint32_t*>(p) = bits; }
 __device__ __forceinline__ void sg_store(__nv_bfloat16* p, uint32_t bits) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)bits; }
 
-// One warp's 32 rows x 128 bytes from staging to global memory: columns [c0, c0 + 128 bytes), of which those under `cols` exist,
-// rows under `rows`.  On 16-byte rows eight lanes send a row of 128 bytes; otherwise a lane sends an element, a row at a time.
+// One warp's 32 rows x 64 bytes: row `lane` to staging as four chunks of 16 bytes, chunk c at c ^ (row / 2) % 4 (eight rows then fall on
+// different banks), and from there to global memory: columns from c0, of which those under `cols` exist, rows under `rows`.  On
+// 16-byte rows four lanes send a row's 64 bytes; otherwise a lane sends an element, a row (bf16) or two (fp32) at a time.
+__device__ __forceinline__ uint32_t sg_staged(uint32_t stg, int r, int c) { return stg + (uint32_t)r * 64u + (uint32_t)((c ^ ((r >> 1) & 3)) << 4); }
+__device__ __forceinline__ void sg_stage(uint32_t stg, int lane, int c, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sg_staged(stg, lane, c)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 template <typename T>
 __device__ __forceinline__ void sg_rows_out(uint32_t stg, T* out, int64_t ld, int rows, int c0, int cols, bool vec, int lane) {
-    constexpr int PER = 16 / sizeof(T), WIDE = 128 / sizeof(T);
+    constexpr int PER = 16 / sizeof(T), WIDE = 64 / sizeof(T);
     if (vec) {
-        const int c = c0 + (lane & 7) * PER;
+        const int c = c0 + (lane & 3) * PER;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3);
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + (lane >> 2);
             if (r < rows && c < cols) {  // rows of out are whole chunks: so are cols
                 uint4 v;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                             : "r"(stg + (uint32_t)r * 128u + (uint32_t)(((lane & 7) ^ (r & 7)) << 4)) : "memory");
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(sg_staged(stg, r, lane & 3)) : "memory");
                 *reinterpret_cast<uint4*>(out + r * ld + c) = v;
             }
         }
         return;
     }
-    for (int r = 0; r < rows; ++r)
-#pragma unroll
-        for (int h = 0; h < WIDE / 32; ++h) {
-            const int e = lane + 32 * h;
-            if (c0 + e < cols) {
-                const uint32_t at = stg + (uint32_t)r * 128u + (uint32_t)(((e / PER) ^ (r & 7)) << 4) + (uint32_t)(e % PER) * (uint32_t)sizeof(T);
-                uint32_t v;
-                if (sizeof(T) == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-                else { uint16_t h16; asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h16) : "r"(at) : "memory"); v = h16; }
-                sg_store(out + r * ld + c0 + e, v);
-            }
-        }
+    const int e = lane % WIDE;
+    if (c0 + e >= cols) return;
+    for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
+        const uint32_t at = sg_staged(stg, r, e / PER) + (uint32_t)(e % PER) * (uint32_t)sizeof(T);
+        uint32_t v;
+        if (sizeof(T) == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+        else { uint16_t h16; asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h16) : "r"(at) : "memory"); v = h16; }
+        sg_store(out + r * ld + c0 + e, v);
+    }
 }
 
-// rows of no segment: zeros, by the epilogue warps (threads 64 .. 319 of each block)
-template <typename T>
+// rows of no segment: zeros, by the epilogue warps (threads from 64 on)
+template <int WARPS, typename T>
 __device__ __forceinline__ void sg_zero_outside(const SegGemmParams& P, T* out) {
     const int64_t p0 = seg_at(P, 0) * P.cols_out, p1 = seg_at(P, P.G) * P.cols_out, end = P.N * P.cols_out;
-    const int64_t me = (int64_t)blockIdx.x * (32 * SG_EPI_WARPS) + ((int)threadIdx.x - 64), all = (int64_t)gridDim.x * (32 * SG_EPI_WARPS);
+    const int64_t me = (int64_t)blockIdx.x * (32 * WARPS) + ((int)threadIdx.x - 64), all = (int64_t)gridDim.x * (32 * WARPS);
     for (int64_t i = me; i < p0; i += all) out[i] = T(0.f);
     for (int64_t i = p1 + me; i < end; i += all) out[i] = T(0.f);
 }
 
-// 32 accumulator columns of this warp's 32 rows
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
-    tmem_ld16(taddr, r);
-    tmem_ld16(taddr + 16, r + 16);
+// int32 -> fp32, one rounding.  The conversion instruction runs at a quarter of the rate of additions: every other value goes by its
+// halves, each exact in fp32 (low 16 bits on top of 2^23, high ones on 1.5 * 2^23), joined by one fma.
+__device__ __forceinline__ float sg_int_float(int x, bool halves) {
+    if (!halves) return (float)x;
+    const float lo = __uint_as_float(0x4B000000u | ((uint32_t)x & 0xFFFFu)) - 8388608.f;
+    const float hi = __int_as_float(0x4B400000 + (x >> 16)) - 12582912.f;
+    return fmaf(hi, 65536.f, lo);
 }
 
 template <int MODE, typename T>
@@ -253,27 +304,27 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             const int slices = slices_of(t);
             for (int j = 0; j < slices; ++j, ++it) {
                 const int s = (int)(it % (uint32_t)S);
-                bool ok = true;
-                if (lane == 0) {
-                    ok = mbar_wait_bounded(empty(s), ((it / (uint32_t)S) & 1u) ^ 1u);
-                    if (ok) {
-                        mbar_arrive_expect_tx(full(s), a_box + b_bytes);
-                        const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
-                        if constexpr (MODE == SG_DW) {
-                            const int row = (int)(t.lo + (int64_t)j * 64);
-                            for (int h = 0; h < 2; ++h) sg_load(a0 + (uint32_t)h * 8192u, &mapA, mb * 128 + h * 64, row, 0, full(s), once);
-                            for (int h = 0; h < bn / 64; ++h) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, 0, full(s), once);
-                        } else {
-                            constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
-                            sg_load(a0, &mapA, j * STEP, (int)t.lo, 0, full(s), once);
-                            if constexpr (MODE == SG_Y)
-                                for (int h = 0; h < bn / 64; ++h) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, t.g, full(s), keep);
-                            else
-                                sg_load(b0, &mapB, j * STEP, nb * bn, t.g, full(s), keep);
-                        }
+                if (!sg_wait(empty(s), ((it / (uint32_t)S) & 1u) ^ 1u)) { failed = true; return false; }
+                sg_expect(full(s), a_box + b_bytes);
+                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
+                if constexpr (MODE == SG_DW) {
+                    const int row = (int)(t.lo + (int64_t)j * 64);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) sg_load(a0 + (uint32_t)h * 8192u, &mapA, mb * 128 + h * 64, row, 0, full(s), once);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (h * 64 < bn) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, 0, full(s), once);
+                } else {
+                    constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
+                    sg_load(a0, &mapA, j * STEP, (int)t.lo, 0, full(s), once);
+                    if constexpr (MODE == SG_Y) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            if (h * 64 < bn) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, t.g, full(s), keep);
+                    } else {
+                        sg_load(b0, &mapB, j * STEP, nb * bn, t.g, full(s), keep);
                     }
                 }
-                if (!__shfl_sync(0xFFFFFFFFu, (int)ok, 0)) { failed = true; return false; }
             }
             return true;
         });
@@ -289,16 +340,14 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             const uint32_t a = lt & 1u;
             const uint32_t dacc = tmem_base + a * acc_cols;
             const int slices = slices_of(t);
-            bool ok = lane != 0 || mbar_wait_bounded(acc_empty(a), ((lt >> 1) & 1u) ^ 1u);
+            if (!sg_wait(acc_empty(a), ((lt >> 1) & 1u) ^ 1u)) { failed = true; return false; }
             for (int j = 0; j < slices; ++j, ++it) {
                 const int s = (int)(it % (uint32_t)S);
                 const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
-                if (lane == 0 && ok) ok = mbar_wait_bounded(full(s), (it / (uint32_t)S) & 1u);
-                if (!__shfl_sync(0xFFFFFFFFu, (int)ok, 0)) { failed = true; return false; }
+                if (!sg_wait(full(s), (it / (uint32_t)S) & 1u)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {
                     const int have = (int)(t.hi - t.lo - (int64_t)j * 64);
                     if (have < 64) {  // rows of the next segment: 128 bytes each, from `have` to the end of every box
-                        mbar_wait_bounded(full(s), (it / (uint32_t)S) & 1u);  // (has completed: orders every lane's stores behind the copies)
                         for (int box = 0; box < 2 + bn / 64; ++box)
                             for (uint32_t o = (uint32_t)have * 128u + (uint32_t)lane * 16u; o < 8192u; o += 512u)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a0 + (uint32_t)box * 8192u + o), "r"(0u) : "memory");
@@ -306,30 +355,30 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         __syncwarp();
                     }
                 }
-                if (lane == 0) {
-                    tc_fence_after();
+                tc_fence_after();
+                // K-major: rows 128 bytes apart, groups of 8 rows 1024, a k-step 32 bytes along the row.  MN-major: 16
+                // contraction rows of 128 bytes a k-step, boxes of 64 columns 8192 bytes apart.  A k-step adds a constant to
+                // the descriptors' address field (units of 16 bytes)
+                constexpr bool A_MN = MODE == SG_DW, B_MN = MODE == SG_DW || MODE == SG_Y;
+                const uint64_t ad = make_smem_desc(a0, A_MN ? 8192 : 16, 1024, SG_SW128), bd = make_smem_desc(b0, B_MN ? 8192 : 16, 1024, SG_SW128);
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        // K-major: rows 128 bytes apart, groups of 8 rows 1024, a k-step 32 bytes along the row.  MN-major: 16
-                        // contraction rows of 128 bytes a k-step, boxes of 64 columns 8192 bytes apart
-                        const uint64_t ad = MODE == SG_DW ? make_smem_desc(a0 + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
-                                                          : make_smem_desc(a0 + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
-                        const uint64_t bd = MODE == SG_DW || MODE == SG_Y ? make_smem_desc(b0 + (uint32_t)kk * 2048u, 8192, 1024, SG_SW128)
-                                                                          : make_smem_desc(b0 + (uint32_t)kk * 32u, 16, 1024, SG_SW128);
-                        const uint32_t more = j > 0 || kk > 0;
-                        if constexpr (MODE == SG_I8) mma_i8_ss(dacc, ad, bd, idesc, more);
-                        else mma_bf16_ss(dacc, ad, bd, idesc, more);
-                    }
-                    mma_commit(empty(s));
+                for (int kk = 0; kk < 4; ++kk) {
+                    const uint64_t da = ad + (uint64_t)(kk * (A_MN ? 128 : 2)), db = bd + (uint64_t)(kk * (B_MN ? 128 : 2));
+                    const uint32_t more = kk > 0 ? 1u : j > 0;
+                    if constexpr (MODE == SG_I8) sg_mma_i8(dacc, da, db, idesc, more);
+                    else sg_mma_bf16(dacc, da, db, idesc, more);
                 }
-                __syncwarp();
+                sg_commit(empty(s));
             }
-            if (lane == 0) mma_commit(acc_full(a));
+            sg_commit(acc_full(a));
             ++lt;
             return true;
         });
+        // every commit has arrived before the CTA leaves
+        if (lane == 0)
+            for (uint32_t i = it > (uint32_t)S ? it - (uint32_t)S : 0u; i < it; ++i) mbar_wait_bounded(empty((int)(i % (uint32_t)S)), (i / (uint32_t)S) & 1u);
     } else {
-        const int ew = warp - 2, quarter = warp & 3, half = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
+        const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
         uint32_t lt = 0;
         int staged_g = -1, staged_n = -1;
@@ -337,64 +386,71 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             const uint32_t a = lt & 1u;
             if (MODE != SG_DW && (P.bias || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                s_cols[0][c] = P.bias && c < bn && col < P.cols_out ? P.bias[(int64_t)t.g * P.cols_out + col] : 0.f;
-                if constexpr (MODE == SG_I8) s_cols[1][c] = c < bn && col < P.cols_out ? P.sw[col] : 0.f;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                asm volatile("bar.sync 1, 512;" ::: "memory");
+                if (c < 256) {
+                    s_cols[0][c] = P.bias && c < bn && col < P.cols_out ? P.bias[(int64_t)t.g * P.cols_out + col] : 0.f;
+                    if constexpr (MODE == SG_I8) s_cols[1][c] = c < bn && col < P.cols_out ? P.sw[col] : 0.f;
+                }
+                asm volatile("bar.sync 1, 512;" ::: "memory");
                 staged_g = t.g;
                 staged_n = nb;
             }
-            if (!mbar_wait_bounded(acc_full(a), (lt >> 1) & 1u)) { failed = true; return false; }
+            if (!sg_wait(acc_full(a), (lt >> 1) & 1u)) { failed = true; return false; }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
             const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - t.lo - quarter * 32;
             const int rows = (int)(left < 32 ? left : 32);
-            const bool cut = MODE == SG_DW && (seg_at(P, t.g) != t.lo || seg_at(P, t.g + 1) != t.hi);
+            const bool cut = MODE == SG_DW && (t.a != t.lo || t.b != t.hi);
             const int c_base = nb * bn, c_end = P.cols_out;
             float sx = 0.f;
             if (MODE == SG_I8 && lane < rows) sx = P.sx[t.lo + quarter * 32 + lane];
-            // 32 columns at c -> fp32 values
-            auto fetch = [&](int c, float* f) {
-                uint32_t r[32];
-                tmem_ld32(taddr + (uint32_t)c, r);
-                tmem_ld_wait();
+            // 16 columns at c -> fp32 values, two at a time
+            auto finish = [&](int c, const uint32_t* r, float* f) {
 #pragma unroll
-                for (int q = 0; q < 32; ++q) f[q] = MODE == SG_I8 ? (float)(int)r[q] : __uint_as_float(r[q]);
-                if constexpr (MODE == SG_I8) {
+                for (int q = 0; q < 16; ++q) f[q] = MODE == SG_I8 ? sg_int_float((int)r[q], q & 1) : __uint_as_float(r[q]);
 #pragma unroll
-                    for (int q = 0; q < 32; q += 4) {
+                for (int q = 0; q < 16; q += 4) {
+                    float2 u = make_float2(f[q], f[q + 1]), v = make_float2(f[q + 2], f[q + 3]);
+                    const float2 nil = make_float2(-0.f, -0.f);
+                    if constexpr (MODE == SG_I8) {
                         const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c + q]);
-                        f[q] *= sx * w.x; f[q + 1] *= sx * w.y; f[q + 2] *= sx * w.z; f[q + 3] *= sx * w.w;
+                        const float2 x = make_float2(sx, sx);
+                        u = fma2(u, fma2(x, make_float2(w.x, w.y), nil), nil);
+                        v = fma2(v, fma2(x, make_float2(w.z, w.w), nil), nil);
                     }
-                }
-                if (MODE != SG_DW && P.bias) {
-#pragma unroll
-                    for (int q = 0; q < 32; q += 4) {
+                    if (MODE != SG_DW && P.bias) {
                         const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
-                        f[q] += b.x; f[q + 1] += b.y; f[q + 2] += b.z; f[q + 3] += b.w;
+                        u = add2(u, make_float2(b.x, b.y));
+                        v = add2(v, make_float2(b.z, b.w));
                     }
+                    f[q] = u.x; f[q + 1] = u.y; f[q + 2] = v.x; f[q + 3] = v.y;
                 }
-                if (MODE != SG_DW && P.relu) {
+            };
+            auto relu = [&](auto one, uint4 v) {  // of rounded values, as of the sums; a NaN stays
+                if (MODE == SG_DW || !P.relu) return v;
+                uint32_t* const w = &v.x;
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) f[q] = f[q] < 0.f ? 0.f : f[q];  // NaN stays
-                }
+                for (int q = 0; q < 4; ++q)
+                    if constexpr (sizeof(one) == 4) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(*reinterpret_cast<float*>(w + q)));
+                    else asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[q]) : "r"(0u));
+                return v;
             };
             auto send = [&](auto* out, int64_t ld, bool vec) {
                 using O = typename std::remove_pointer<decltype(out)>::type;
-                constexpr int WIDE = 128 / sizeof(O), CH = 32 * sizeof(O) / 16;  // columns of a staging row; chunks of 32 columns
-                for (int cb = half; cb * WIDE < bn; cb += 2) {
+                constexpr int WIDE = 64 / sizeof(O);  // columns of a staging row: 16 or 32
+                for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
                     if (c_base + cb * WIDE >= c_end || rows <= 0) break;  // the whole warp
+                    uint32_t r[WIDE];
+#pragma unroll
+                    for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
+                    tmem_ld_wait();
                     __syncwarp();
 #pragma unroll
-                    for (int h = 0; h < WIDE / 32; ++h) {
-                        float f[32];
-                        fetch(cb * WIDE + h * 32, f);
+                    for (int h = 0; h < WIDE / 16; ++h) {
+                        float f[16];
+                        finish(cb * WIDE + h * 16, r + h * 16, f);
 #pragma unroll
-                        for (int q = 0; q < CH; ++q) {
-                            const uint4 v = Chunk<O>::pack(f + q * Chunk<O>::N);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stg + (uint32_t)lane * 128u + (uint32_t)(((h * CH + q) ^ (lane & 7)) << 4)),
-                                         "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-                        }
+                        for (int q = 0; q < 16 / Chunk<O>::N; ++q) sg_stage(stg, lane, h * (16 / Chunk<O>::N) + q, relu(O(), Chunk<O>::pack(f + q * Chunk<O>::N)));
                     }
                     __syncwarp();
                     sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
@@ -405,7 +461,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                 const int64_t size = (int64_t)P.rows_out * P.cols_out;
                 if (cut) {
                     // cut at the part's start: partial 2p, else (at its end) 2p + 1
-                    const int64_t which = 2 * part + (seg_at(P, t.g) >= part * P.part_rows ? 1 : 0);
+                    const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
                     send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0);
                 } else {
                     send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0);
@@ -419,7 +475,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             ++lt;
             return true;
         });
-        if (MODE == SG_Y || MODE == SG_DX) sg_zero_outside(P, (T*)P.out);
+        if (MODE == SG_Y || MODE == SG_DX) sg_zero_outside<SG_EPI_WARPS>(P, (T*)P.out);
     }
     if (failed) atomicExch(P.status, 7);  // GNN_ERR_TIMEOUT
     tc_fence_before();

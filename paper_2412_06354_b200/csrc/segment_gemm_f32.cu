@@ -20,8 +20,8 @@
 
 namespace gnn {
 
-constexpr int SF_CONV_WARPS = 8, SF_GROUPS = 2, SF_GROUP_WARPS = SF_CONV_WARPS / SF_GROUPS;
-constexpr int SF_THREADS = SG_THREADS + 32 * SF_CONV_WARPS;
+constexpr int SF_EPI_WARPS = 8, SF_CONV_WARPS = 8, SF_GROUPS = 2, SF_GROUP_WARPS = SF_CONV_WARPS / SF_GROUPS;
+constexpr int SF_THREADS = 32 * (2 + SF_EPI_WARPS + SF_CONV_WARPS);
 constexpr int SF_RAW_SLOTS = 4, SF_B_SLOTS = 4;  // at most
 
 struct SegGemmF32Layout {
@@ -86,7 +86,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         for (uint32_t s = 0; s < nraw; ++s) { mbar_init(r_full(s), 1); mbar_init(r_empty(s), SF_GROUP_WARPS); }
         for (uint32_t s = 0; s < nb_slots; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), 1); }
         for (uint32_t o = 0; o < SF_GROUPS; ++o) { mbar_init(o_full(o), SF_GROUP_WARPS); mbar_init(o_empty(o), 1); }
-        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SG_EPI_WARPS); }
+        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SF_EPI_WARPS); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
@@ -116,39 +116,36 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         sg_walk<MODE>(P, [&](const SegRows& t, int mb, int nb, int64_t) {
             const int slices = slices_of(t);
             for (int j = 0; j < slices; ++j, ++it) {
-                bool ok = true;
-                if (lane == 0) {
-                    const uint32_t s = it % nraw;
-                    const uint32_t to = raw0 + s * L.raw_bytes;
-                    ok = mbar_wait_bounded(r_empty(s), ((it / nraw) & 1u) ^ 1u);
-                    if (ok) {
-                        if constexpr (MODE == SG_DW) {  // boxes of 32 rows x 32 columns
-                            mbar_arrive_expect_tx(r_full(s), (uint32_t)(4 + bn / 32) * 4096u);
-                            const int row = (int)(t.lo + (int64_t)j * SLICE);
-                            for (int h = 0; h < 4; ++h) sg_load(to + (uint32_t)h * 4096u, &mapA, mb * 128 + h * 32, row, 0, r_full(s), once);
-                            for (int h = 0; h < bn / 32; ++h) sg_load(to + (uint32_t)(4 + h) * 4096u, &mapB, nb * bn + h * 32, row, 0, r_full(s), once);
-                        } else {  // two boxes of 32 columns, one where the contraction ends in the first
-                            const int boxes = have_of(t, j) > 32 ? 2 : 1;
-                            mbar_arrive_expect_tx(r_full(s), (uint32_t)(boxes * P.a_rows) * 128u);
-                            for (int h = 0; h < boxes; ++h) sg_load(to + (uint32_t)h * SG_A_BYTES, &mapA, j * SLICE + h * 32, (int)t.lo, 0, r_full(s), once);
-                        }
-                    }
-                    if (MODE != SG_DW && ok) {
-                        const uint32_t q = it % nb_slots;
-                        ok = mbar_wait_bounded(b_empty(q), ((it / nb_slots) & 1u) ^ 1u);
-                        if (ok) {
-                            mbar_arrive_expect_tx(b_full(q), L.b_bytes);
-                            const uint32_t bs = b0 + q * L.b_bytes;
-                            for (int l = 0; l < 3; ++l)
-                                if constexpr (MODE == SG_Y)
-                                    for (int h = 0; h < bn / 64; ++h)
-                                        sg_load(bs + (uint32_t)l * b_level + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * SLICE, l * P.G + t.g, b_full(q), keep);
-                                else
-                                    sg_load(bs + (uint32_t)l * b_level, &mapB, j * SLICE, nb * bn, l * P.G + t.g, b_full(q), keep);
+                const uint32_t s = it % nraw, to = raw0 + s * L.raw_bytes;
+                if (!sg_wait(r_empty(s), ((it / nraw) & 1u) ^ 1u)) { failed = true; return false; }
+                if constexpr (MODE == SG_DW) {  // boxes of 32 rows x 32 columns
+                    sg_expect(r_full(s), (uint32_t)(4 + bn / 32) * 4096u);
+                    const int row = (int)(t.lo + (int64_t)j * SLICE);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) sg_load(to + (uint32_t)h * 4096u, &mapA, mb * 128 + h * 32, row, 0, r_full(s), once);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (h * 32 < bn) sg_load(to + (uint32_t)(4 + h) * 4096u, &mapB, nb * bn + h * 32, row, 0, r_full(s), once);
+                } else {  // two boxes of 32 columns, one where the contraction ends in the first
+                    const bool two = have_of(t, j) > 32;
+                    sg_expect(r_full(s), (uint32_t)((two ? 2 : 1) * P.a_rows) * 128u);
+                    sg_load(to, &mapA, j * SLICE, (int)t.lo, 0, r_full(s), once);
+                    if (two) sg_load(to + SG_A_BYTES, &mapA, j * SLICE + 32, (int)t.lo, 0, r_full(s), once);
+                    const uint32_t q = it % nb_slots;
+                    if (!sg_wait(b_empty(q), ((it / nb_slots) & 1u) ^ 1u)) { failed = true; return false; }
+                    sg_expect(b_full(q), L.b_bytes);
+                    const uint32_t bs = b0 + q * L.b_bytes;
+#pragma unroll
+                    for (int l = 0; l < 3; ++l) {
+                        if constexpr (MODE == SG_Y) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                if (h * 64 < bn) sg_load(bs + (uint32_t)l * b_level + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * SLICE, l * P.G + t.g, b_full(q), keep);
+                        } else {
+                            sg_load(bs + (uint32_t)l * b_level, &mapB, j * SLICE, nb * bn, l * P.G + t.g, b_full(q), keep);
                         }
                     }
                 }
-                if (!__shfl_sync(0xFFFFFFFFu, (int)ok, 0)) { failed = true; return false; }
             }
             return true;
         });
@@ -162,43 +159,45 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         const uint32_t idesc = make_idesc(bn, MODE != SG_DX, 0);
         uint32_t it = 0, lt = 0;
         sg_walk<MODE>(P, [&](const SegRows& t, int, int, int64_t) {
-            const uint32_t a = lt % nacc, dacc = tmem_base + a * acc_cols;
+            const uint32_t a = lt % nacc, dacc = tmem_base + a * acc_cols, small = dacc + (uint32_t)bn;
             const int slices = slices_of(t);
-            bool ok = lane != 0 || mbar_wait_bounded(acc_empty(a), ((lt / nacc) & 1u) ^ 1u);
+            if (!sg_wait(acc_empty(a), ((lt / nacc) & 1u) ^ 1u)) { failed = true; return false; }
             for (int j = 0; j < slices; ++j, ++it) {
-                if (lane == 0 && ok) {
-                    const uint32_t o = it % SF_GROUPS, q = MODE == SG_DW ? o : it % nb_slots;
-                    ok = mbar_wait_bounded(o_full(o), (it / SF_GROUPS) & 1u);
-                    if (MODE != SG_DW && ok) ok = mbar_wait_bounded(b_full(q), (it / nb_slots) & 1u);
-                    if (ok) {
-                        tc_fence_after();
-                        const uint32_t at = op0 + o * OP_COLS, bs = b0 + q * L.b_bytes;
-                        const int steps = (have_of(t, j) + 15) / 16;
+                const uint32_t o = it % SF_GROUPS, q = MODE == SG_DW ? o : it % nb_slots;
+                if (!sg_wait(o_full(o), (it / SF_GROUPS) & 1u)) { failed = true; return false; }
+                if (MODE != SG_DW && !sg_wait(b_full(q), (it / nb_slots) & 1u)) { failed = true; return false; }
+                tc_fence_after();
+                const uint32_t at = op0 + o * OP_COLS;
+                // MN-major: boxes of 64 columns, SLICE contraction rows of 128 bytes each; K-major: rows of 64.  Levels and
+                // k-steps add to the descriptor's address field (units of 16 bytes)
+                const uint64_t bd = MODE == SG_DX ? make_smem_desc(b0 + q * L.b_bytes, 16, 1024, SG_SW128)
+                                                  : make_smem_desc(b0 + q * L.b_bytes, SLICE * 128, 1024, SG_SW128);
+                const uint64_t level[3] = {bd, bd + b_level / 16, bd + b_level / 8};
+                const int steps = (have_of(t, j) + 15) / 16;
 #pragma unroll
-                        for (int kk = 0; kk < SLICE / 16; ++kk) {
-                            if (kk >= steps) break;
+                for (int kk = 0; kk < SLICE / 16; ++kk) {
+                    if (kk >= steps) break;
 #pragma unroll
-                            for (int p = 0; p < 6; ++p) {
-                                const uint32_t bl = bs + sf_pair_b(p) * b_level;
-                                // MN-major: boxes of 64 columns, SLICE contraction rows of 128 bytes each; K-major: rows of 64
-                                const uint64_t bd = MODE == SG_DX ? make_smem_desc(bl + (uint32_t)kk * 32u, 16, 1024, SG_SW128)
-                                                                  : make_smem_desc(bl + (uint32_t)kk * 2048u, SLICE * 128, 1024, SG_SW128);
-                                const uint32_t more = j > 0 || kk > 0 || (p > 0 && p < 5);
-                                mma_bf16_ts(dacc + (p < 5 ? (uint32_t)bn : 0u), at + sf_pair_a(p) * OP_LEVEL + (uint32_t)kk * 8u, bd, idesc, more);
-                            }
-                        }
-                        mma_commit(o_empty(o));
-                        if (MODE != SG_DW) mma_commit(b_empty(q));
+                    for (int p = 0; p < 6; ++p) {
+                        const uint32_t more = kk > 0 || (p > 0 && p < 5) ? 1u : j > 0;
+                        sg_mma_bf16_ts(p < 5 ? small : dacc, at + (sf_pair_a(p) * OP_LEVEL + (uint32_t)kk * 8u), level[sf_pair_b(p)] + (uint64_t)(kk * (MODE == SG_DX ? 2 : 128)), idesc, more);
                     }
                 }
-                if (!__shfl_sync(0xFFFFFFFFu, (int)ok, 0)) { failed = true; return false; }
+                sg_commit(o_empty(o));
+                if (MODE != SG_DW) sg_commit(b_empty(q));
             }
-            if (lane == 0) mma_commit(acc_full(a));
+            sg_commit(acc_full(a));
             ++lt;
             return true;
         });
-    } else if (warp >= 2 + SG_EPI_WARPS) {
-        const uint32_t grp = (uint32_t)(warp - 2 - SG_EPI_WARPS) / SF_GROUP_WARPS;
+        // every commit has arrived before the CTA leaves
+        if (lane == 0) {
+            for (uint32_t i = it > SF_GROUPS ? it - SF_GROUPS : 0u; i < it; ++i) mbar_wait_bounded(o_empty(i % SF_GROUPS), (i / SF_GROUPS) & 1u);
+            if (MODE != SG_DW)
+                for (uint32_t i = it > nb_slots ? it - nb_slots : 0u; i < it; ++i) mbar_wait_bounded(b_empty(i % nb_slots), (i / nb_slots) & 1u);
+        }
+    } else if (warp >= 2 + SF_EPI_WARPS) {
+        const uint32_t grp = (uint32_t)(warp - 2 - SF_EPI_WARPS) / SF_GROUP_WARPS;
         const int quarter = warp & 3;  // a warp reaches the 32 lanes of tensor memory of its number modulo 4
         uint32_t it = 0;
         sg_walk<MODE>(P, [&](const SegRows& t, int, int, int64_t) {
@@ -206,24 +205,30 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             for (int j = 0; j < slices; ++j, ++it) {
                 if (it % SF_GROUPS != grp) continue;
                 const uint32_t s = it % nraw;
-                if (!mbar_wait_bounded(r_full(s), (it / nraw) & 1u) || !mbar_wait_bounded(o_empty(grp), ((it / SF_GROUPS) & 1u) ^ 1u)) { failed = true; return false; }
+                if (!sg_wait(r_full(s), (it / nraw) & 1u) || !sg_wait(o_empty(grp), ((it / SF_GROUPS) & 1u) ^ 1u)) { failed = true; return false; }
                 tc_fence_after();
                 const uint32_t from = raw0 + s * L.raw_bytes;
                 const uint32_t to = op0 + ((uint32_t)(quarter * 32) << 16) + grp * OP_COLS;
                 const int have = have_of(t, j);
                 if constexpr (MODE != SG_DW) {
                     const uint32_t r = (uint32_t)(quarter * 32 + lane), x7 = r & 7u;
+                    // a box of 32 columns at a time: all its loads before the first split
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {  // 8 elements of row r
-                        if (c * 8 >= have) break;
-                        const uint32_t at = from + (uint32_t)(c >> 2) * SG_A_BYTES + r * 128u;
-                        float x[8];
-                        sf_read16(at + (((uint32_t)(2 * (c & 3)) ^ x7) << 4), x);
-                        sf_read16(at + (((uint32_t)(2 * (c & 3) + 1) ^ x7) << 4), x + 4);
-                        uint4 lv[3];
-                        sf_split(x, lv);
+                    for (int h = 0; h < 2; ++h) {
+                        if (h * 32 >= have) break;
+                        const uint32_t at = from + (uint32_t)h * SG_A_BYTES + r * 128u;
+                        float x[32];
 #pragma unroll
-                        for (int l = 0; l < 3; ++l) tmem_st4(to + (uint32_t)l * OP_LEVEL + (uint32_t)c * 4u, lv[l]);
+                        for (int c = 0; c < 8; ++c) sf_read16(at + (((uint32_t)c ^ x7) << 4), x + 4 * c);
+                        const int chunks = (have - h * 32 + 7) / 8;  // of 8 elements; the box is zeros past the last
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (c >= chunks) break;
+                            uint4 lv[3];
+                            sf_split(x + 8 * c, lv);
+#pragma unroll
+                            for (int l = 0; l < 3; ++l) tmem_st4(to + (uint32_t)l * OP_LEVEL + (uint32_t)(h * 16 + c * 4), lv[l]);
+                        }
                     }
                     if (const int c = (have + 7) / 8; c & 1) {  // the second half of the last k-step: zeros
 #pragma unroll
@@ -273,7 +278,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             return true;
         });
     } else {
-        const int ew = warp - 2, quarter = warp & 3, half = ew >> 2;
+        const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
         uint32_t lt = 0;
         int staged_g = -1, staged_n = -1;
@@ -287,7 +292,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
                 staged_g = t.g;
                 staged_n = nb;
             }
-            if (!mbar_wait_bounded(acc_full(a), (lt / nacc) & 1u)) { failed = true; return false; }
+            if (!sg_wait(acc_full(a), (lt / nacc) & 1u)) { failed = true; return false; }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
             const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - t.lo - quarter * 32;
@@ -296,9 +301,9 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             bool vec = P.vec != 0;
             if constexpr (MODE == SG_DW) {
                 const int64_t size = (int64_t)P.rows_out * P.cols_out;
-                if (seg_at(P, t.g) != t.lo || seg_at(P, t.g + 1) != t.hi) {
+                if (t.a != t.lo || t.b != t.hi) {
                     // cut at the part's start: partial 2p, else (at its end) 2p + 1
-                    out = P.part + (2 * part + (seg_at(P, t.g) >= part * P.part_rows ? 1 : 0)) * size;
+                    out = P.part + (2 * part + (t.a >= part * P.part_rows ? 1 : 0)) * size;
                     vec = P.cols_out % 4 == 0;
                 } else {
                     out += t.g * size;
@@ -307,33 +312,28 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             } else {
                 out += (t.lo + quarter * 32) * P.cols_out;
             }
-            for (int cb = half; cb * 32 < bn; cb += 2) {
-                if (c_base + cb * 32 >= P.cols_out || rows <= 0) break;  // the whole warp
-                __syncwarp();
+            for (int cb = sub; cb * 16 < bn; cb += SF_EPI_WARPS / 4) {
+                if (c_base + cb * 16 >= P.cols_out || rows <= 0) break;  // the whole warp
+                uint32_t r[16], m[16];
+                tmem_ld16(taddr + (uint32_t)(cb * 16), r);
+                tmem_ld16(taddr + (uint32_t)(bn + cb * 16), m);
+                tmem_ld_wait();
+                float f[16];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t r[16], m[16];
-                    tmem_ld16(taddr + (uint32_t)(cb * 32 + h * 16), r);
-                    tmem_ld16(taddr + (uint32_t)(bn + cb * 32 + h * 16), m);
-                    tmem_ld_wait();
-                    float f[16];
+                for (int q = 0; q < 16; ++q) f[q] = __uint_as_float(r[q]) + __uint_as_float(m[q]);
+                if (MODE == SG_Y && P.bias) {
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) f[q] = __uint_as_float(r[q]) + __uint_as_float(m[q]);
-                    if (MODE == SG_Y && P.bias) {
+                    for (int q = 0; q < 16; ++q) f[q] += s_bias[cb * 16 + q];
+                }
+                if (MODE == SG_Y && P.relu) {
 #pragma unroll
-                        for (int q = 0; q < 16; ++q) f[q] += s_bias[cb * 32 + h * 16 + q];
-                    }
-                    if (MODE == SG_Y && P.relu) {
-#pragma unroll
-                        for (int q = 0; q < 16; ++q) f[q] = f[q] < 0.f ? 0.f : f[q];  // NaN stays
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stg + (uint32_t)lane * 128u + (uint32_t)(((h * 4 + q) ^ (lane & 7)) << 4)),
-                                     "r"(__float_as_uint(f[4 * q])), "r"(__float_as_uint(f[4 * q + 1])), "r"(__float_as_uint(f[4 * q + 2])), "r"(__float_as_uint(f[4 * q + 3])) : "memory");
+                    for (int q = 0; q < 16; ++q) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(f[q]));  // NaN stays
                 }
                 __syncwarp();
-                sg_rows_out<float>(stg, out, P.cols_out, rows, c_base + cb * 32, P.cols_out, vec, lane);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sg_stage(stg, lane, q, Chunk<float>::pack(f + 4 * q));
+                __syncwarp();
+                sg_rows_out<float>(stg, out, P.cols_out, rows, c_base + cb * 16, P.cols_out, vec, lane);
             }
             tc_fence_before();
             __syncwarp();
@@ -341,7 +341,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             ++lt;
             return true;
         });
-        if (MODE != SG_DW) sg_zero_outside(P, (float*)P.out);
+        if (MODE != SG_DW) sg_zero_outside<SF_EPI_WARPS>(P, (float*)P.out);
     }
     if (failed) atomicExch(P.status, 7);  // GNN_ERR_TIMEOUT
     tc_fence_before();
@@ -354,7 +354,7 @@ static gnn_status sf_launch(const char* who, int which, const CUtensorMap& mapA,
     const auto kernel = segment_gemm_f32_kernel<MODE>;
     const gnn_status rc = allow_big_smem(who, (const void*)kernel, which, SG_SMEM_MAX);
     if (rc != GNN_OK) return rc;
-    const size_t fixed = SG_EPI_WARPS * SG_STAGING;
+    const size_t fixed = SF_EPI_WARPS * SG_STAGING;
     SegGemmF32Layout L;
     // tensor memory: accumulators of 2 bn columns, twice where 512 columns hold them beside a slice of A per group
     constexpr int OPS = SF_GROUPS * 3 * (MODE == SG_DW ? 16 : 32);
