@@ -248,8 +248,7 @@ linear_i8_rows_kernel(const int8_t* xq, const float* sx, const int8_t* wq, const
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (lane != r || n0 + r >= N) continue;
-        float y = (float)acc[r] * (sx[n0 + r] * sw[m]);
-        if (bias) y += bias[m];
+        float y = fmaf((float)acc[r] * sx[n0 + r], sw[m], bias ? bias[m] : 0.f);  // as the tensor-core path rounds
         if (relu) y = y < 0.f ? 0.f : y;
         Y[(int64_t)(n0 + r) * M + m] = T(y);
     }
@@ -345,7 +344,7 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     P.seg_ptr = nullptr; P.G = 1; P.N = N;
     P.bn = sg_block(M, 256, row_tiles);
     P.tiles_n = (M + P.bn - 1) / P.bn; P.tiles_m = 1;
-    P.units = row_tiles * P.tiles_n;
+    sg_deal(P, (size_t)K * M);
     P.slices = (K + 127) / 128; P.contraction = K;
     P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
     P.rows_out = TC_ROWS; P.cols_out = M;

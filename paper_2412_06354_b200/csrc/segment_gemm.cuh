@@ -8,11 +8,17 @@
 //
 // Rows of segment g are seg_ptr[g] .. seg_ptr[g+1]-1, known on the device only: no size is read back.
 //
-// Tiles of SG_Y, SG_DX and SG_I8: 128 rows of ONE segment x bn output columns.  A tile's number leads to its segment without a
-// prefix sum: floor(seg_ptr[g] / 128) + g is strictly increasing in g and leaves every segment at least ceil(rows / 128)
-// numbers, so tile s belongs to the last g whose number is not above s (a warp compares 32 segments at a time); at most G of
-// the N / 128 + G numbers are empty.  A tile's 128 rows may reach into the next segment: the products of those rows are
+// Tiles of SG_Y, SG_DX and SG_I8: 128 rows of ONE segment x bn output columns.  A block number leads to its segment without a
+// prefix sum: floor(seg_ptr[g] / R) + g is strictly increasing in g and leaves every segment at least ceil(rows / R) numbers, so
+// block s of R rows belongs to the last g whose number is not above s (a warp compares 32 segments at a time); at most G of
+// the N / R + G numbers are empty.  A tile's 128 rows may reach into the next segment: the products of those rows are
 // computed and not stored.
+//   ranges > 0: every CTA takes one block of columns of a range of consecutive blocks of 32 rows, equally many for each, and cuts
+//               it into tiles as the segments ask.  Its weights stay in shared memory as long as the segment does (where the
+//               contraction is short enough: `resident` buffers of them), so that the ring brings rows alone, and CTAs end together:
+//               170,000 x 128 -> 128, 1334 tiles dealt out to 148 SMs one by one: a tenth round for a few.
+//   otherwise:  tiles of 128 rows dealt out, all columns of a tile side by side: neighbouring CTAs share a segment's weights in L2, which
+//               could not hold all segments' at once; and where there are few rows.
 // SG_DW: the rows are cut into equal parts, whatever the segments; a CTA takes one block [128 features x bn columns] of the
 // result over one part and finishes it for each segment that it meets there.  A segment that lies in one part is written at
 // once; one that is cut leaves an fp32 partial per part (two per part at most: the segment cut at its start, the one cut at
@@ -43,7 +49,7 @@ enum { SG_Y = 0, SG_DX = 1, SG_DW = 2, SG_I8 = 3 };
 
 constexpr int SG_EPI_WARPS = 16;
 constexpr int SG_THREADS = 32 * (2 + SG_EPI_WARPS);
-constexpr int SG_MAX_STAGES = 8;
+constexpr int SG_MAX_STAGES = 10;
 constexpr size_t SG_SMEM_MAX = 224 * 1024;      // dynamic; with the static part on its 1024-byte boundary: the 227 KB of a block
 constexpr uint32_t SG_A_BYTES = 128 * 128;      // 128 rows of 128 bytes (SG_DW: two boxes of 64 features x 64 rows)
 constexpr uint32_t SG_STAGING = 32 * 64;        // per epilogue warp: 32 rows of 64 bytes
@@ -53,7 +59,8 @@ struct SegGemmParams {
     const int64_t* seg_ptr;  // [G+1], or nullptr: one segment of all rows
     int G;
     int64_t N;
-    int64_t units;           // tiles (SG_DW: parts x blocks of the result)
+    int64_t units;           // tiles, or ranges x blocks of columns (SG_DW: parts x blocks of the result)
+    int ranges, resident;    // see above
     int slices, contraction; // (not SG_DW) slices of the contraction, its elements
     int tiles_n, tiles_m;    // blocks of output columns; of features (SG_DW)
     int bn;                  // output columns of a tile: a multiple of 64, at most 256, fp32 128
@@ -101,25 +108,25 @@ __device__ __forceinline__ SegFound last_segment(const SegGemmParams& P, F befor
         hi = min(hi, lo + step);
     }
 }
-// Tile number s -> its rows (hi <= lo: none), for ascending s: the segment of the last tile is kept, so that most tiles are two
-// comparisons and an addition.  (Searching anew for each, with 64-bit divisions, the loader took 3400 cycles a tile and was the bound
-// of 170,000 x 128 -> 128.)
+// Block number s of 2^SHIFT rows -> its segment and first row, for ascending s: the segment of the last one is kept, so that most
+// are two comparisons and an addition.  (Searching anew for each, with 64-bit divisions, took the loader 1000 cycles a tile.)
+template <int SHIFT>
 struct SegCursor {
     int g;
-    int64_t a, b, first, next;  // rows of segment g, its tile numbers
-    __device__ __forceinline__ SegCursor() : g(0), a(0), b(0), first(0), next(0) {}
-    __device__ __forceinline__ SegRows tile(const SegGemmParams& P, int64_t s) {
+    int64_t a, b, first, next;  // rows of segment g, its block numbers
+    __device__ __forceinline__ SegCursor() : g(-1), a(0), b(0), first(0), next(0) {}
+    // first row of block s; g < 0: before the first segment
+    __device__ __forceinline__ int64_t at(const SegGemmParams& P, int64_t s) {
         if (s >= next) {
-            const SegFound f = last_segment(P, [&](int q, int64_t v) { return (v >> 7) + q <= s; });
-            if (f.g < 0) return {0, 0, 0, 0, 0};
+            const SegFound f = last_segment(P, [&](int q, int64_t v) { return (v >> SHIFT) + q <= s; });
+            if (f.g < 0) return 0;
             g = f.g;
             a = f.a;
             b = f.b;
-            first = (a >> 7) + g;
-            next = (b >> 7) + g + 1;  // (of the next segment; not above the true bound where seg_ptr descends)
+            first = (a >> SHIFT) + g;
+            next = (b >> SHIFT) + g + 1;  // (of the next segment; not above the true bound where seg_ptr descends)
         }
-        const int64_t lo = a + ((s - first) << 7);
-        return {lo, lo + TC_ROWS < b ? lo + TC_ROWS : b, g, a, b};
+        return a + ((s - first) << SHIFT);
     }
 };
 
@@ -167,15 +174,37 @@ __device__ __forceinline__ uint64_t policy_normal() {
 // it says stop.
 template <int MODE, class Body>
 __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
-    if constexpr (MODE != SG_DW) {
-        // unit = tile number * tiles_n + block of columns
+    if (MODE != SG_DW && P.ranges > 0) {
+        // unit = range of consecutive blocks of 32 rows * tiles_n + block of columns
+        const int64_t blocks = (P.N >> 5) + P.G;
+        for (unsigned u = blockIdx.x; u < (unsigned)P.units; u += gridDim.x) {
+            const int n = (int)(u % (unsigned)P.tiles_n);
+            const unsigned r = u / (unsigned)P.tiles_n;
+            const int64_t s1 = blocks * (r + 1) / P.ranges;
+            SegCursor<5> at;
+            for (int64_t s = blocks * r / P.ranges; s < s1;) {
+                const int64_t lo = at.at(P, s);
+                if (at.g < 0 || lo >= at.b) {  // rows of no segment before the first one, the empty block at a segment's end
+                    s = at.g < 0 ? (seg_at(P, 0) >> 5) > s ? (seg_at(P, 0) >> 5) : s + 1 : at.next > s ? at.next : s + 1;
+                    continue;
+                }
+                int64_t hi = lo + TC_ROWS < at.b ? lo + TC_ROWS : at.b;
+                const int64_t end = at.a + ((s1 - at.first) << 5);  // what follows belongs to the next range
+                if (hi > end) hi = end;
+                if (!body(SegRows{lo, hi, at.g, at.a, at.b}, 0, n, (int64_t)0)) return;
+                s = s + (TC_ROWS >> 5) < at.next ? s + (TC_ROWS >> 5) : at.next > s ? at.next : s + 1;
+            }
+        }
+    } else if constexpr (MODE != SG_DW) {
+        // unit = number of a tile of 128 rows * tiles_n + block of columns
         const unsigned nn = (unsigned)P.tiles_n, ds = gridDim.x / nn, dn = gridDim.x % nn;
         unsigned n = blockIdx.x % nn;
         int64_t s = blockIdx.x / nn;
-        SegCursor at;
+        SegCursor<7> at;
         for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
-            const SegRows t = at.tile(P, s);
-            if (t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            const int64_t lo = at.at(P, s);
+            const SegRows t = {lo, lo + TC_ROWS < at.b ? lo + TC_ROWS : at.b, at.g, at.a, at.b};
+            if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
             s += ds;
             n += dn;
             if (n >= nn) { n -= nn; ++s; }
@@ -257,7 +286,7 @@ template <int MODE, typename T>
 __global__ void __launch_bounds__(SG_THREADS, 1)
 segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const SegGemmParams P) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzle atoms lie on 1024 bytes
-    __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 4];  // full[S], empty[S], acc_full[2], acc_empty[2]
+    __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 8];  // full[S], empty[S], acc_full[2], acc_empty[2], b_full[2], b_empty[2]
     __shared__ __align__(16) float s_cols[MODE == SG_I8 ? 2 : 1][256];                 // bias and column scales of the tile, zeros past the last
     __shared__ uint32_t tmem_base_slot;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -268,17 +297,20 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         return;
     }
     const uint32_t b_bytes = (uint32_t)bn * 128u;
-    const uint32_t slot_bytes = SG_A_BYTES + b_bytes;
-    const uint32_t stage0 = base, ring0 = base + SG_EPI_WARPS * SG_STAGING;
+    const int nres = MODE == SG_DW ? 0 : P.resident;
+    const uint32_t slot_bytes = SG_A_BYTES + (nres ? 0u : b_bytes), b_tile = (uint32_t)P.slices * b_bytes;
+    const uint32_t stage0 = base, res0 = base + SG_EPI_WARPS * SG_STAGING, ring0 = res0 + (uint32_t)nres * b_tile;
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
     auto empty = [&](int s) { return bar0 + 8u * (uint32_t)(SG_MAX_STAGES + s); };
     auto acc_full = [&](uint32_t a) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + a); };
     auto acc_empty = [&](uint32_t a) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 2 + a); };
+    auto b_full = [&](uint32_t b) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 4 + b); };
+    auto b_empty = [&](uint32_t b) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 6 + b); };
 
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SG_EPI_WARPS); }
+        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SG_EPI_WARPS); mbar_init(b_full(a), 1); mbar_init(b_empty(a), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
@@ -298,14 +330,34 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
     if (warp == 0) {
         const uint64_t keep = policy_evict_last(), once = P.tiles_n > 1 || P.tiles_m > 1 ? policy_normal() : policy_evict_first();
-        uint32_t it = 0;
+        uint32_t it = 0, loads = 0;  // slices; sets of resident weights
+        int held_g = -1, held_n = -1;
         const uint32_t a_box = MODE == SG_DW ? SG_A_BYTES : (uint32_t)P.a_rows * 128u;
+        constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
+        auto load_b = [&](uint32_t to, int j, int g, int nb, uint32_t bar) {
+            if constexpr (MODE == SG_Y) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (h * 64 < bn) sg_load(to + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, g, bar, keep);
+            } else {
+                sg_load(to, &mapB, j * STEP, nb * bn, g, bar, keep);
+            }
+        };
         walk([&](const SegRows& t, int mb, int nb, int64_t) {
             const int slices = slices_of(t);
+            if (nres && (t.g != held_g || nb != held_n)) {
+                const uint32_t b = loads % (uint32_t)nres;
+                if (!sg_wait(b_empty(b), ((loads / (uint32_t)nres) & 1u) ^ 1u)) { failed = true; return false; }
+                sg_expect(b_full(b), b_tile);
+                for (int j = 0; j < slices; ++j) load_b(res0 + b * b_tile + (uint32_t)j * b_bytes, j, t.g, nb, b_full(b));
+                ++loads;
+                held_g = t.g;
+                held_n = nb;
+            }
             for (int j = 0; j < slices; ++j, ++it) {
                 const int s = (int)(it % (uint32_t)S);
                 if (!sg_wait(empty(s), ((it / (uint32_t)S) & 1u) ^ 1u)) { failed = true; return false; }
-                sg_expect(full(s), a_box + b_bytes);
+                sg_expect(full(s), nres ? a_box : a_box + b_bytes);
                 const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
                 if constexpr (MODE == SG_DW) {
                     const int row = (int)(t.lo + (int64_t)j * 64);
@@ -315,15 +367,8 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     for (int h = 0; h < 4; ++h)
                         if (h * 64 < bn) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, 0, full(s), once);
                 } else {
-                    constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
                     sg_load(a0, &mapA, j * STEP, (int)t.lo, 0, full(s), once);
-                    if constexpr (MODE == SG_Y) {
-#pragma unroll
-                        for (int h = 0; h < 4; ++h)
-                            if (h * 64 < bn) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, j * 64, t.g, full(s), keep);
-                    } else {
-                        sg_load(b0, &mapB, j * STEP, nb * bn, t.g, full(s), keep);
-                    }
+                    if (!nres) load_b(b0, j, t.g, nb, full(s));
                 }
             }
             return true;
@@ -332,18 +377,28 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             // do not leave while copies into this CTA's shared memory may still be in flight
             const uint32_t first = it > (uint32_t)S ? it - (uint32_t)S : 0u;
             for (uint32_t i = first; i < it; ++i) mbar_wait_bounded(full((int)(i % (uint32_t)S)), (i / (uint32_t)S) & 1u);
+            for (uint32_t i = loads > (uint32_t)nres ? loads - (uint32_t)nres : 0u; i < loads; ++i) mbar_wait_bounded(b_full(i % (uint32_t)nres), (i / (uint32_t)nres) & 1u);
         }
     } else if (warp == 1) {
         const uint32_t idesc = MODE == SG_I8 ? make_idesc_i8(bn) : make_idesc(bn, MODE != SG_DX, MODE == SG_DW);
-        uint32_t it = 0, lt = 0;
-        walk([&](const SegRows& t, int, int, int64_t) {
+        uint32_t it = 0, lt = 0, loads = 0;
+        int held_g = -1, held_n = -1;
+        walk([&](const SegRows& t, int, int nb, int64_t) {
+            if (nres && (t.g != held_g || nb != held_n)) {
+                if (loads > 0) sg_commit(b_empty((loads - 1) % (uint32_t)nres));  // the products of the last set are done
+                if (!sg_wait(b_full(loads % (uint32_t)nres), (loads / (uint32_t)nres) & 1u)) { failed = true; return false; }
+                ++loads;
+                held_g = t.g;
+                held_n = nb;
+            }
+            const uint32_t res = nres ? res0 + (loads - 1) % (uint32_t)nres * b_tile : 0u;
             const uint32_t a = lt & 1u;
             const uint32_t dacc = tmem_base + a * acc_cols;
             const int slices = slices_of(t);
             if (!sg_wait(acc_empty(a), ((lt >> 1) & 1u) ^ 1u)) { failed = true; return false; }
             for (int j = 0; j < slices; ++j, ++it) {
                 const int s = (int)(it % (uint32_t)S);
-                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
+                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = nres ? res + (uint32_t)j * b_bytes : a0 + SG_A_BYTES;
                 if (!sg_wait(full(s), (it / (uint32_t)S) & 1u)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {
                     const int have = (int)(t.hi - t.lo - (int64_t)j * 64);
@@ -374,7 +429,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             ++lt;
             return true;
         });
-        // every commit has arrived before the CTA leaves
+        // every commit has arrived before the CTA leaves (those of resident weights before later ones of the ring)
         if (lane == 0)
             for (uint32_t i = it > (uint32_t)S ? it - (uint32_t)S : 0u; i < it; ++i) mbar_wait_bounded(empty((int)(i % (uint32_t)S)), (i / (uint32_t)S) & 1u);
     } else {
@@ -406,19 +461,26 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             if (MODE == SG_I8 && lane < rows) sx = P.sx[t.lo + quarter * 32 + lane];
             // 16 columns at c -> fp32 values, two at a time
             auto finish = [&](int c, const uint32_t* r, float* f) {
+                if (MODE == SG_I8 && P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
 #pragma unroll
-                for (int q = 0; q < 16; ++q) f[q] = MODE == SG_I8 ? sg_int_float((int)r[q], q & 1) : __uint_as_float(r[q]);
+                    for (int q = 0; q < 16; q += 2) {
+                        const float2 u = add2(make_float2(__uint_as_float(r[q] + 0x4B400000u), __uint_as_float(r[q + 1] + 0x4B400000u)), make_float2(-12582912.f, -12582912.f));
+                        f[q] = u.x; f[q + 1] = u.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) f[q] = MODE == SG_I8 ? sg_int_float((int)r[q], q & 1) : __uint_as_float(r[q]);
+                }
 #pragma unroll
                 for (int q = 0; q < 16; q += 4) {
                     float2 u = make_float2(f[q], f[q + 1]), v = make_float2(f[q + 2], f[q + 3]);
                     const float2 nil = make_float2(-0.f, -0.f);
-                    if constexpr (MODE == SG_I8) {
-                        const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c + q]);
+                    if constexpr (MODE == SG_I8) {  // (zeros where there is no bias)
+                        const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c + q]), b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
                         const float2 x = make_float2(sx, sx);
-                        u = fma2(u, fma2(x, make_float2(w.x, w.y), nil), nil);
-                        v = fma2(v, fma2(x, make_float2(w.z, w.w), nil), nil);
-                    }
-                    if (MODE != SG_DW && P.bias) {
+                        u = fma2(fma2(u, x, nil), make_float2(w.x, w.y), make_float2(b.x, b.y));
+                        v = fma2(fma2(v, x, nil), make_float2(w.z, w.w), make_float2(b.z, b.w));
+                    } else if (MODE != SG_DW && P.bias) {
                         const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
                         u = add2(u, make_float2(b.x, b.y));
                         v = add2(v, make_float2(b.z, b.w));
@@ -500,18 +562,29 @@ inline int sg_block(int cols, int most, int64_t row_tiles) {
     return bn;
 }
 
+// How the tiles of SG_Y, SG_DX and SG_I8 are dealt out (see above): ranges where all weights together are a fraction of L2 and the rows
+// give every SM a few tiles.
+inline void sg_deal(SegGemmParams& P, size_t weight_bytes) {
+    const int64_t row_tiles = P.N / TC_ROWS + P.G;
+    P.ranges = weight_bytes <= ((size_t)32 << 20) && P.N / TC_ROWS * P.tiles_n >= 296 && P.G <= P.N / 512 && P.tiles_n <= 148 ? 148 / P.tiles_n : 0;
+    P.units = (P.ranges ? P.ranges : row_tiles) * P.tiles_n;
+}
+
 template <int MODE, typename T>
 static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st) {
     const auto kernel = segment_gemm_kernel<MODE, T>;
     const gnn_status rc = allow_big_smem(who, (const void*)kernel, which, SG_SMEM_MAX);
     if (rc != GNN_OK) return rc;
-    const size_t fixed = SG_EPI_WARPS * SG_STAGING, slot = SG_A_BYTES + (size_t)P.bn * 128;
-    int stages = (int)((SG_SMEM_MAX - fixed) / slot);
+    const size_t fixed = SG_EPI_WARPS * SG_STAGING, b_bytes = (size_t)P.bn * 128, tile = MODE == SG_DW ? 0 : b_bytes * P.slices;
+    // resident weights: two sets where they leave the ring eight slots, one where they leave it four
+    P.resident = MODE != SG_DW && P.ranges > 0 ? (fixed + 2 * tile + 8 * SG_A_BYTES <= SG_SMEM_MAX ? 2 : fixed + tile + 4 * SG_A_BYTES <= SG_SMEM_MAX ? 1 : 0) : 0;
+    const size_t slot = SG_A_BYTES + (P.resident ? 0 : b_bytes), held = (size_t)P.resident * tile;
+    int stages = (int)((SG_SMEM_MAX - fixed - held) / slot);
     P.stages = stages > SG_MAX_STAGES ? SG_MAX_STAGES : stages;
     int cols = 32;
     while (cols < 2 * P.bn) cols <<= 1;
     P.tmem_cols = cols;
-    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SG_THREADS), fixed + (size_t)P.stages * slot, st, mapA, mapB, P);
+    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SG_THREADS), fixed + held + (size_t)P.stages * slot, st, mapA, mapB, P);
     GNN_CHECK_LAUNCH(who);
     return GNN_OK;
 }

@@ -261,3 +261,23 @@ def test_gradients_against_differences(gnn):
         # each Y is off by at most 1e-5 of its terms' absolute sum (under 1e-5 * K * |x||w|), summed with |dY| over both calls
         room = 1e-5 * float((dY.double().abs() * (up.abs() + down.abs() + 40)).sum()) / (2 * h) + 1e-5 * float((grad.double().cpu().abs() * V.abs().double()).sum() + 40)
         assert abs(slope - want) <= room
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,M", [(64, 64), (128, 200), (300, 128)])
+def test_rows_by_consecutive_ranges(gnn, dtype, K, M):
+    """Rows enough for every SM, few segments: ends of ranges and of segments in all places, segments of one row and none among
+    long ones, rows of no segment on both sides."""
+    import torch
+    sizes = [9000, 1, 0, 127, 14001, 1, 1, 5000, 0, 33, 12800]
+    X, ptr, W, b, dY = data(dtype, sizes, K, M, lead=77, tail=1203, seed=K)
+    Xd, pd, Wd, bd, dYd = (t.cuda() for t in (X, ptr, W, b, dY))
+    Y, ws = gnn.linear_segments(Xd, pd, Wd, bias=bd, relu=True, return_ws=True)
+    assert status(ws) == 0
+    ref, S = forward_ref(X, ptr, W, b, True)
+    close(Y, ref, S, "relu(Y + b)")
+    dX, dW, ws = gnn.linear_segments_backward(Xd, pd, Wd, dYd, return_ws=True)
+    assert status(ws) == 0
+    rX, SX, rW, SW = backward_ref(X, ptr, W, dY)
+    close(dX, rX, SX, "dX")
+    close(dW, rW, SW, "dW")
