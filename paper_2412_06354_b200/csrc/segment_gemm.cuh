@@ -170,6 +170,11 @@ __device__ __forceinline__ uint64_t policy_normal() {
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
+// seg_ptr on its way to L2 while the kernel before still runs (a hint: nothing of it is used before pdl_wait)
+__device__ __forceinline__ void sg_touch(const SegGemmParams& P) {
+    if (P.seg_ptr && blockIdx.x == 0 && (int)threadIdx.x * 16 <= P.G) asm volatile("prefetch.global.L2 [%0];" ::"l"(P.seg_ptr + threadIdx.x * 16));
+}
+
 // Every role of a CTA walks the same pieces of work: body(rows of one segment, block of features, block of columns, part) until
 // it says stop.
 template <int MODE, class Body>
@@ -241,15 +246,20 @@ template <typename T>
 __device__ __forceinline__ void sg_rows_out(uint32_t stg, T* out, int64_t ld, int rows, int c0, int cols, bool vec, int lane) {
     constexpr int PER = 16 / sizeof(T), WIDE = 64 / sizeof(T);
     if (vec) {
-        const int c = c0 + (lane & 3) * PER;
+        const int c = c0 + (lane & 3) * PER, r0 = lane >> 2;
+        T* to = out + r0 * ld + c;
+        const int64_t step = 8 * ld;
+        uint4 v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 8 + (lane >> 2);
-            if (r < rows && c < cols) {  // rows of out are whole chunks: so are cols
-                uint4 v;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(sg_staged(stg, r, lane & 3)) : "memory");
-                *reinterpret_cast<uint4*>(out + r * ld + c) = v;
-            }
+        for (int i = 0; i < 4; ++i)  // (row + 8: the same place of its chunks)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(sg_staged(stg, r0, lane & 3) + (uint32_t)i * 512u) : "memory");
+        if (rows == 32 && c0 + WIDE <= cols) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i, to += step) *reinterpret_cast<uint4*>(to) = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i, to += step)
+                if (r0 + 8 * i < rows && c < cols) *reinterpret_cast<uint4*>(to) = v[i];  // rows of out are whole chunks: so are cols
         }
         return;
     }
@@ -282,6 +292,25 @@ __device__ __forceinline__ float sg_int_float(int x, bool halves) {
     return fmaf(hi, 65536.f, lo);
 }
 
+// a chunk of 16 bytes, max(., 0) with the rounding; a NaN stays
+template <bool RELU>
+__device__ __forceinline__ uint4 sg_pack(const float*, const float* f) {
+    float g[4] = {f[0], f[1], f[2], f[3]};
+    if (RELU) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(g[q]));
+    }
+    return Chunk<float>::pack(g);
+}
+template <bool RELU>
+__device__ __forceinline__ uint4 sg_pack(const __nv_bfloat16*, const float* f) {
+    if (!RELU) return Chunk<__nv_bfloat16>::pack(f);
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(f[2 * q + 1]), "f"(f[2 * q]));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 template <int MODE, typename T>
 __global__ void __launch_bounds__(SG_THREADS, 1)
 segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const SegGemmParams P) {
@@ -297,7 +326,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         return;
     }
     const uint32_t b_bytes = (uint32_t)bn * 128u;
-    const int nres = MODE == SG_DW ? 0 : P.resident;
+    const int nres = P.resident;  // (SG_DW: 0)
     const uint32_t slot_bytes = SG_A_BYTES + (nres ? 0u : b_bytes), b_tile = (uint32_t)P.slices * b_bytes;
     const uint32_t stage0 = base, res0 = base + SG_EPI_WARPS * SG_STAGING, ring0 = res0 + (uint32_t)nres * b_tile;
     const uint32_t bar0 = smem_u32(bars);
@@ -315,6 +344,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
     }
+    sg_touch(P);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base_slot), (uint32_t)P.tmem_cols);
     tc_fence_before();
     __syncthreads();
@@ -345,7 +375,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         };
         walk([&](const SegRows& t, int mb, int nb, int64_t) {
             const int slices = slices_of(t);
-            if (nres && (t.g != held_g || nb != held_n)) {
+            if (MODE != SG_DW && nres && (t.g != held_g || nb != held_n)) {
                 const uint32_t b = loads % (uint32_t)nres;
                 if (!sg_wait(b_empty(b), ((loads / (uint32_t)nres) & 1u) ^ 1u)) { failed = true; return false; }
                 sg_expect(b_full(b), b_tile);
@@ -439,7 +469,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         int staged_g = -1, staged_n = -1;
         walk([&](const SegRows& t, int mb, int nb, int64_t part) {
             const uint32_t a = lt & 1u;
-            if (MODE != SG_DW && (P.bias || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
+            if ((MODE == SG_Y || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
                 asm volatile("bar.sync 1, 512;" ::: "memory");
                 if (c < 256) {
@@ -459,60 +489,46 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             const int c_base = nb * bn, c_end = P.cols_out;
             float sx = 0.f;
             if (MODE == SG_I8 && lane < rows) sx = P.sx[t.lo + quarter * 32 + lane];
-            // 16 columns at c -> fp32 values, two at a time
-            auto finish = [&](int c, const uint32_t* r, float* f) {
-                if (MODE == SG_I8 && P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
+            // four sums at column c of the tile -> values before relu
+            auto finish4 = [&](int c, const uint32_t* r, float* f) {
+                if constexpr (MODE == SG_I8) {
+                    const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c]), b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
+                    const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int q = 0; q < 16; q += 2) {
-                        const float2 u = add2(make_float2(__uint_as_float(r[q] + 0x4B400000u), __uint_as_float(r[q + 1] + 0x4B400000u)), make_float2(-12582912.f, -12582912.f));
-                        f[q] = u.x; f[q + 1] = u.y;
-                    }
+                    for (int q = 0; q < 4; ++q) f[q] = fmaf(f[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
+                } else if constexpr (MODE == SG_Y) {
+                    const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
+                    f[0] = __uint_as_float(r[0]) + b.x; f[1] = __uint_as_float(r[1]) + b.y; f[2] = __uint_as_float(r[2]) + b.z; f[3] = __uint_as_float(r[3]) + b.w;
                 } else {
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) f[q] = MODE == SG_I8 ? sg_int_float((int)r[q], q & 1) : __uint_as_float(r[q]);
-                }
-#pragma unroll
-                for (int q = 0; q < 16; q += 4) {
-                    float2 u = make_float2(f[q], f[q + 1]), v = make_float2(f[q + 2], f[q + 3]);
-                    const float2 nil = make_float2(-0.f, -0.f);
-                    if constexpr (MODE == SG_I8) {  // (zeros where there is no bias)
-                        const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c + q]), b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
-                        const float2 x = make_float2(sx, sx);
-                        u = fma2(fma2(u, x, nil), make_float2(w.x, w.y), make_float2(b.x, b.y));
-                        v = fma2(fma2(v, x, nil), make_float2(w.z, w.w), make_float2(b.z, b.w));
-                    } else if (MODE != SG_DW && P.bias) {
-                        const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c + q]);
-                        u = add2(u, make_float2(b.x, b.y));
-                        v = add2(v, make_float2(b.z, b.w));
-                    }
-                    f[q] = u.x; f[q + 1] = u.y; f[q + 2] = v.x; f[q + 3] = v.y;
+                    for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(r[q]);
                 }
             };
-            auto relu = [&](auto one, uint4 v) {  // of rounded values, as of the sums; a NaN stays
-                if (MODE == SG_DW || !P.relu) return v;
-                uint32_t* const w = &v.x;
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if constexpr (sizeof(one) == 4) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(*reinterpret_cast<float*>(w + q)));
-                    else asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[q]) : "r"(0u));
-                return v;
-            };
-            auto send = [&](auto* out, int64_t ld, bool vec) {
+            auto send = [&](auto* out, int64_t ld, bool vec, auto with_relu) {
                 using O = typename std::remove_pointer<decltype(out)>::type;
-                constexpr int WIDE = 64 / sizeof(O);  // columns of a staging row: 16 or 32
+                constexpr int WIDE = 64 / sizeof(O), PER = Chunk<O>::N;  // columns of a staging row: 16 or 32; of a chunk
                 for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
                     if (c_base + cb * WIDE >= c_end || rows <= 0) break;  // the whole warp
                     uint32_t r[WIDE];
 #pragma unroll
                     for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
                     tmem_ld_wait();
+                    float f[WIDE];
+                    if constexpr (MODE == SG_I8) {
+                        if (P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
+#pragma unroll
+                            for (int q = 0; q < WIDE; ++q) f[q] = __uint_as_float(r[q] + 0x4B400000u) - 12582912.f;
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < WIDE; ++q) f[q] = sg_int_float((int)r[q], q & 1);
+                        }
+                    }
                     __syncwarp();
 #pragma unroll
-                    for (int h = 0; h < WIDE / 16; ++h) {
-                        float f[16];
-                        finish(cb * WIDE + h * 16, r + h * 16, f);
+                    for (int q = 0; q < WIDE / PER; ++q) {
 #pragma unroll
-                        for (int q = 0; q < 16 / Chunk<O>::N; ++q) sg_stage(stg, lane, h * (16 / Chunk<O>::N) + q, relu(O(), Chunk<O>::pack(f + q * Chunk<O>::N)));
+                        for (int k = 0; k < PER; k += 4) finish4(cb * WIDE + q * PER + k, r + q * PER + k, f + q * PER + k);
+                        sg_stage(stg, lane, q, sg_pack<decltype(with_relu)::value>((O*)nullptr, f + q * PER));
                     }
                     __syncwarp();
                     sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
@@ -524,12 +540,14 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                 if (cut) {
                     // cut at the part's start: partial 2p, else (at its end) 2p + 1
                     const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
-                    send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0);
+                    send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0, std::false_type());
                 } else {
-                    send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0);
+                    send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0, std::false_type());
                 }
             } else {
-                send((T*)P.out + (t.lo + quarter * 32) * P.cols_out, P.cols_out, P.vec != 0);
+                T* const to = (T*)P.out + (t.lo + quarter * 32) * P.cols_out;
+                if (MODE != SG_DX && P.relu) send(to, P.cols_out, P.vec != 0, std::true_type());
+                else send(to, P.cols_out, P.vec != 0, std::false_type());
             }
             tc_fence_before();
             __syncwarp();

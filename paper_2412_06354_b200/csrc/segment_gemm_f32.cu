@@ -91,6 +91,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
     }
+    sg_touch(P);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base_slot), 512);
     tc_fence_before();
     __syncthreads();
