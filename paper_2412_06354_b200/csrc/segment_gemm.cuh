@@ -61,6 +61,7 @@ struct SegGemmParams {
     int64_t N;
     int64_t units;           // tiles, or ranges x blocks of columns (SG_DW: parts x blocks of the result)
     int ranges, resident;    // see above
+    unsigned per_range, longer;
     int slices, contraction; // (not SG_DW) slices of the contraction, its elements
     int tiles_n, tiles_m;    // blocks of output columns; of features (SG_DW)
     int bn;                  // output columns of a tile: a multiple of 64, at most 256, fp32 128
@@ -132,6 +133,21 @@ struct SegCursor {
 
 // a bounded wait of a whole warp, with one answer
 __device__ __forceinline__ bool sg_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity)); }
+// a place in a ring of n slots and the parity of its round (counted, not divided: n is known at run time only)
+struct SgRing {
+    uint32_t n, s, parity, uses;
+    __device__ __forceinline__ explicit SgRing(int slots) : n((uint32_t)slots), s(0), parity(0), uses(0) {}
+    __device__ __forceinline__ void next() {
+        ++uses;
+        if (++s == n) { s = 0; parity ^= 1u; }
+    }
+    // waits for the last use of every slot: bar(slot)
+    template <class F>
+    __device__ __forceinline__ void drain(F bar) const {
+        for (uint32_t q = 0; q < n; ++q)
+            if (q < s || uses >= n) mbar_wait_bounded(bar(q), q < s ? parity : parity ^ 1u);
+    }
+};
 // What one thread of a warp does, called by the whole warp: the election stands in the instruction itself, so that the control flow
 // around it stays that of a whole warp.  (As a branch of lane 0 around loops of them, copies took 250 cycles each to issue and MMAs
 // 85.)  The same thread is elected every time.
@@ -180,14 +196,14 @@ __device__ __forceinline__ void sg_touch(const SegGemmParams& P) {
 template <int MODE, class Body>
 __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
     if (MODE != SG_DW && P.ranges > 0) {
-        // unit = range of consecutive blocks of 32 rows * tiles_n + block of columns
-        const int64_t blocks = (P.N >> 5) + P.G;
+        // unit = range of consecutive blocks of 32 rows * tiles_n + block of columns; a range is per_range blocks, the first ones of a
+        // remainder one more.  (No 64-bit division: a microsecond of a CTA's start.)
         for (unsigned u = blockIdx.x; u < (unsigned)P.units; u += gridDim.x) {
-            const int n = (int)(u % (unsigned)P.tiles_n);
-            const unsigned r = u / (unsigned)P.tiles_n;
-            const int64_t s1 = blocks * (r + 1) / P.ranges;
+            const unsigned r = P.tiles_n == 1 ? u : u / (unsigned)P.tiles_n;
+            const int n = (int)(u - r * (unsigned)P.tiles_n);
+            const int64_t s0 = r * P.per_range + (r < P.longer ? r : P.longer), s1 = s0 + P.per_range + (r < P.longer ? 1u : 0u);
             SegCursor<5> at;
-            for (int64_t s = blocks * r / P.ranges; s < s1;) {
+            for (int64_t s = s0; s < s1;) {
                 const int64_t lo = at.at(P, s);
                 if (at.g < 0 || lo >= at.b) {  // rows of no segment before the first one, the empty block at a segment's end
                     s = at.g < 0 ? (seg_at(P, 0) >> 5) > s ? (seg_at(P, 0) >> 5) : s + 1 : at.next > s ? at.next : s + 1;
@@ -360,7 +376,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
     if (warp == 0) {
         const uint64_t keep = policy_evict_last(), once = P.tiles_n > 1 || P.tiles_m > 1 ? policy_normal() : policy_evict_first();
-        uint32_t it = 0, loads = 0;  // slices; sets of resident weights
+        SgRing ring(S), sets(nres ? nres : 1);  // slices; sets of resident weights
         int held_g = -1, held_n = -1;
         const uint32_t a_box = MODE == SG_DW ? SG_A_BYTES : (uint32_t)P.a_rows * 128u;
         constexpr int STEP = MODE == SG_I8 ? 128 : 64;  // elements of 128 bytes
@@ -376,17 +392,16 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         walk([&](const SegRows& t, int mb, int nb, int64_t) {
             const int slices = slices_of(t);
             if (MODE != SG_DW && nres && (t.g != held_g || nb != held_n)) {
-                const uint32_t b = loads % (uint32_t)nres;
-                if (!sg_wait(b_empty(b), ((loads / (uint32_t)nres) & 1u) ^ 1u)) { failed = true; return false; }
-                sg_expect(b_full(b), b_tile);
-                for (int j = 0; j < slices; ++j) load_b(res0 + b * b_tile + (uint32_t)j * b_bytes, j, t.g, nb, b_full(b));
-                ++loads;
+                if (!sg_wait(b_empty(sets.s), sets.parity ^ 1u)) { failed = true; return false; }
+                sg_expect(b_full(sets.s), b_tile);
+                for (int j = 0; j < slices; ++j) load_b(res0 + sets.s * b_tile + (uint32_t)j * b_bytes, j, t.g, nb, b_full(sets.s));
+                sets.next();
                 held_g = t.g;
                 held_n = nb;
             }
-            for (int j = 0; j < slices; ++j, ++it) {
-                const int s = (int)(it % (uint32_t)S);
-                if (!sg_wait(empty(s), ((it / (uint32_t)S) & 1u) ^ 1u)) { failed = true; return false; }
+            for (int j = 0; j < slices; ++j, ring.next()) {
+                const int s = (int)ring.s;
+                if (!sg_wait(empty(s), ring.parity ^ 1u)) { failed = true; return false; }
                 sg_expect(full(s), nres ? a_box : a_box + b_bytes);
                 const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
                 if constexpr (MODE == SG_DW) {
@@ -405,31 +420,32 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         });
         if (failed && lane == 0) {
             // do not leave while copies into this CTA's shared memory may still be in flight
-            const uint32_t first = it > (uint32_t)S ? it - (uint32_t)S : 0u;
-            for (uint32_t i = first; i < it; ++i) mbar_wait_bounded(full((int)(i % (uint32_t)S)), (i / (uint32_t)S) & 1u);
-            for (uint32_t i = loads > (uint32_t)nres ? loads - (uint32_t)nres : 0u; i < loads; ++i) mbar_wait_bounded(b_full(i % (uint32_t)nres), (i / (uint32_t)nres) & 1u);
+            ring.drain([&](uint32_t q) { return full((int)q); });
+            sets.drain([&](uint32_t q) { return b_full(q); });
         }
     } else if (warp == 1) {
         const uint32_t idesc = MODE == SG_I8 ? make_idesc_i8(bn) : make_idesc(bn, MODE != SG_DX, MODE == SG_DW);
-        uint32_t it = 0, lt = 0, loads = 0;
+        SgRing ring(S), sets(nres ? nres : 1);
+        uint32_t lt = 0, res = 0, last_set = 0;
         int held_g = -1, held_n = -1;
         walk([&](const SegRows& t, int, int nb, int64_t) {
             if (nres && (t.g != held_g || nb != held_n)) {
-                if (loads > 0) sg_commit(b_empty((loads - 1) % (uint32_t)nres));  // the products of the last set are done
-                if (!sg_wait(b_full(loads % (uint32_t)nres), (loads / (uint32_t)nres) & 1u)) { failed = true; return false; }
-                ++loads;
+                if (sets.uses > 0) sg_commit(b_empty(last_set));  // the products of the last set are done
+                if (!sg_wait(b_full(sets.s), sets.parity)) { failed = true; return false; }
+                last_set = sets.s;
+                res = res0 + last_set * b_tile;
+                sets.next();
                 held_g = t.g;
                 held_n = nb;
             }
-            const uint32_t res = nres ? res0 + (loads - 1) % (uint32_t)nres * b_tile : 0u;
             const uint32_t a = lt & 1u;
             const uint32_t dacc = tmem_base + a * acc_cols;
             const int slices = slices_of(t);
             if (!sg_wait(acc_empty(a), ((lt >> 1) & 1u) ^ 1u)) { failed = true; return false; }
-            for (int j = 0; j < slices; ++j, ++it) {
-                const int s = (int)(it % (uint32_t)S);
+            for (int j = 0; j < slices; ++j, ring.next()) {
+                const int s = (int)ring.s;
                 const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = nres ? res + (uint32_t)j * b_bytes : a0 + SG_A_BYTES;
-                if (!sg_wait(full(s), (it / (uint32_t)S) & 1u)) { failed = true; return false; }
+                if (!sg_wait(full(s), ring.parity)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {
                     const int have = (int)(t.hi - t.lo - (int64_t)j * 64);
                     if (have < 64) {  // rows of the next segment: 128 bytes each, from `have` to the end of every box
@@ -460,8 +476,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             return true;
         });
         // every commit has arrived before the CTA leaves (those of resident weights before later ones of the ring)
-        if (lane == 0)
-            for (uint32_t i = it > (uint32_t)S ? it - (uint32_t)S : 0u; i < it; ++i) mbar_wait_bounded(empty((int)(i % (uint32_t)S)), (i / (uint32_t)S) & 1u);
+        if (lane == 0) ring.drain([&](uint32_t q) { return empty((int)q); });
     } else {
         const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
@@ -586,6 +601,11 @@ inline void sg_deal(SegGemmParams& P, size_t weight_bytes) {
     const int64_t row_tiles = P.N / TC_ROWS + P.G;
     P.ranges = weight_bytes <= ((size_t)32 << 20) && P.N / TC_ROWS * P.tiles_n >= 296 && P.G <= P.N / 512 && P.tiles_n <= 148 ? 148 / P.tiles_n : 0;
     P.units = (P.ranges ? P.ranges : row_tiles) * P.tiles_n;
+    if (P.ranges) {
+        const int64_t blocks = (P.N >> 5) + P.G;
+        P.per_range = (unsigned)(blocks / P.ranges);
+        P.longer = (unsigned)(blocks % P.ranges);
+    }
 }
 
 template <int MODE, typename T>

@@ -104,6 +104,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
     constexpr uint32_t OP_LEVEL = SLICE / 2, OP_COLS = 3 * OP_LEVEL;  // tensor-memory columns of a level, of a slice of A
     const uint32_t op0 = tmem_base + nacc * acc_cols;
     bool failed = false;
+    const bool two_acc = nacc == 2;
     auto slices_of = [&](const SegRows& t) { return MODE == SG_DW ? (int)((t.hi - t.lo + SLICE - 1) / SLICE) : P.slices; };
     // contraction elements of slice j that exist
     auto have_of = [&](const SegRows& t, int j) {
@@ -113,12 +114,12 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
 
     if (warp == 0) {
         const uint64_t keep = policy_evict_last(), once = P.tiles_n > 1 || P.tiles_m > 1 ? policy_normal() : policy_evict_first();
-        uint32_t it = 0;
+        SgRing raw((int)nraw), ws((int)nb_slots);
         sg_walk<MODE>(P, [&](const SegRows& t, int mb, int nb, int64_t) {
             const int slices = slices_of(t);
-            for (int j = 0; j < slices; ++j, ++it) {
-                const uint32_t s = it % nraw, to = raw0 + s * L.raw_bytes;
-                if (!sg_wait(r_empty(s), ((it / nraw) & 1u) ^ 1u)) { failed = true; return false; }
+            for (int j = 0; j < slices; ++j) {
+                const uint32_t s = raw.s, to = raw0 + s * L.raw_bytes;
+                if (!sg_wait(r_empty(s), raw.parity ^ 1u)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {  // boxes of 32 rows x 32 columns
                     sg_expect(r_full(s), (uint32_t)(4 + bn / 32) * 4096u);
                     const int row = (int)(t.lo + (int64_t)j * SLICE);
@@ -132,8 +133,8 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
                     sg_expect(r_full(s), (uint32_t)((two ? 2 : 1) * P.a_rows) * 128u);
                     sg_load(to, &mapA, j * SLICE, (int)t.lo, 0, r_full(s), once);
                     if (two) sg_load(to + SG_A_BYTES, &mapA, j * SLICE + 32, (int)t.lo, 0, r_full(s), once);
-                    const uint32_t q = it % nb_slots;
-                    if (!sg_wait(b_empty(q), ((it / nb_slots) & 1u) ^ 1u)) { failed = true; return false; }
+                    const uint32_t q = ws.s;
+                    if (!sg_wait(b_empty(q), ws.parity ^ 1u)) { failed = true; raw.next(); return false; }
                     sg_expect(b_full(q), L.b_bytes);
                     const uint32_t bs = b0 + q * L.b_bytes;
 #pragma unroll
@@ -146,27 +147,29 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
                             sg_load(bs + (uint32_t)l * b_level, &mapB, j * SLICE, nb * bn, l * P.G + t.g, b_full(q), keep);
                         }
                     }
+                    ws.next();
                 }
+                raw.next();
             }
             return true;
         });
         if (failed && lane == 0) {
-            // do not leave while copies into this CTA's shared memory may still be in flight (slice `it` may have begun)
-            for (uint32_t i = it + 1 > nraw ? it + 1 - nraw : 0u; i <= it; ++i) mbar_wait_bounded(r_full(i % nraw), (i / nraw) & 1u);
-            if (MODE != SG_DW)
-                for (uint32_t i = it > nb_slots ? it - nb_slots : 0u; i < it; ++i) mbar_wait_bounded(b_full(i % nb_slots), (i / nb_slots) & 1u);
+            // do not leave while copies into this CTA's shared memory may still be in flight
+            raw.drain(r_full);
+            if (MODE != SG_DW) ws.drain(b_full);
         }
     } else if (warp == 1) {
         const uint32_t idesc = make_idesc(bn, MODE != SG_DX, 0);
+        SgRing ws((int)nb_slots);
         uint32_t it = 0, lt = 0;
         sg_walk<MODE>(P, [&](const SegRows& t, int, int, int64_t) {
-            const uint32_t a = lt % nacc, dacc = tmem_base + a * acc_cols, small = dacc + (uint32_t)bn;
+            const uint32_t a = two_acc ? lt & 1u : 0u, dacc = tmem_base + a * acc_cols, small = dacc + (uint32_t)bn;
             const int slices = slices_of(t);
-            if (!sg_wait(acc_empty(a), ((lt / nacc) & 1u) ^ 1u)) { failed = true; return false; }
+            if (!sg_wait(acc_empty(a), ((two_acc ? lt >> 1 : lt) & 1u) ^ 1u)) { failed = true; return false; }
             for (int j = 0; j < slices; ++j, ++it) {
-                const uint32_t o = it % SF_GROUPS, q = MODE == SG_DW ? o : it % nb_slots;
+                const uint32_t o = it % SF_GROUPS, q = MODE == SG_DW ? o : ws.s;
                 if (!sg_wait(o_full(o), (it / SF_GROUPS) & 1u)) { failed = true; return false; }
-                if (MODE != SG_DW && !sg_wait(b_full(q), (it / nb_slots) & 1u)) { failed = true; return false; }
+                if (MODE != SG_DW && !sg_wait(b_full(q), ws.parity)) { failed = true; return false; }
                 tc_fence_after();
                 const uint32_t at = op0 + o * OP_COLS;
                 // MN-major: boxes of 64 columns, SLICE contraction rows of 128 bytes each; K-major: rows of 64.  Levels and
@@ -185,7 +188,10 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
                     }
                 }
                 sg_commit(o_empty(o));
-                if (MODE != SG_DW) sg_commit(b_empty(q));
+                if (MODE != SG_DW) {
+                    sg_commit(b_empty(q));
+                    ws.next();
+                }
             }
             sg_commit(acc_full(a));
             ++lt;
@@ -194,19 +200,19 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         // every commit has arrived before the CTA leaves
         if (lane == 0) {
             for (uint32_t i = it > SF_GROUPS ? it - SF_GROUPS : 0u; i < it; ++i) mbar_wait_bounded(o_empty(i % SF_GROUPS), (i / SF_GROUPS) & 1u);
-            if (MODE != SG_DW)
-                for (uint32_t i = it > nb_slots ? it - nb_slots : 0u; i < it; ++i) mbar_wait_bounded(b_empty(i % nb_slots), (i / nb_slots) & 1u);
+            if (MODE != SG_DW) ws.drain(b_empty);
         }
     } else if (warp >= 2 + SF_EPI_WARPS) {
         const uint32_t grp = (uint32_t)(warp - 2 - SF_EPI_WARPS) / SF_GROUP_WARPS;
         const int quarter = warp & 3;  // a warp reaches the 32 lanes of tensor memory of its number modulo 4
+        SgRing raw((int)nraw);
         uint32_t it = 0;
         sg_walk<MODE>(P, [&](const SegRows& t, int, int, int64_t) {
             const int slices = slices_of(t);
-            for (int j = 0; j < slices; ++j, ++it) {
+            for (int j = 0; j < slices; ++j, ++it, raw.next()) {
                 if (it % SF_GROUPS != grp) continue;
-                const uint32_t s = it % nraw;
-                if (!sg_wait(r_full(s), (it / nraw) & 1u) || !sg_wait(o_empty(grp), ((it / SF_GROUPS) & 1u) ^ 1u)) { failed = true; return false; }
+                const uint32_t s = raw.s;
+                if (!sg_wait(r_full(s), raw.parity) || !sg_wait(o_empty(grp), ((it / SF_GROUPS) & 1u) ^ 1u)) { failed = true; return false; }
                 tc_fence_after();
                 const uint32_t from = raw0 + s * L.raw_bytes;
                 const uint32_t to = op0 + ((uint32_t)(quarter * 32) << 16) + grp * OP_COLS;
@@ -284,7 +290,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         uint32_t lt = 0;
         int staged_g = -1, staged_n = -1;
         sg_walk<MODE>(P, [&](const SegRows& t, int mb, int nb, int64_t part) {
-            const uint32_t a = lt % nacc;
+            const uint32_t a = two_acc ? lt & 1u : 0u;
             if (MODE == SG_Y && P.bias && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
                 asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -293,7 +299,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
                 staged_g = t.g;
                 staged_n = nb;
             }
-            if (!sg_wait(acc_full(a), (lt / nacc) & 1u)) { failed = true; return false; }
+            if (!sg_wait(acc_full(a), (two_acc ? lt >> 1 : lt) & 1u)) { failed = true; return false; }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
             const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - t.lo - quarter * 32;
