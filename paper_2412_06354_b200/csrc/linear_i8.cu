@@ -344,8 +344,8 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     P.seg_ptr = nullptr; P.G = 1; P.N = N;
     P.bn = sg_block(M, 256, row_tiles);
     P.tiles_n = (M + P.bn - 1) / P.bn; P.tiles_m = 1;
-    sg_deal(P, (size_t)K * M);
     P.slices = (K + 127) / 128; P.contraction = K;
+    sg_deal(P, (size_t)K * M);
     P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
     P.rows_out = TC_ROWS; P.cols_out = M;
     P.out = Y; P.vec = (size_t)M * elem_size(dtype) % 16 == 0;

@@ -196,8 +196,8 @@ static gnn_status seg_rows(const char* who, bool dx, const void* in, const void*
     P.seg_ptr = seg_ptr; P.G = G; P.N = N;
     P.bn = sg_block(cout, f32 ? 128 : 256, row_tiles);
     P.tiles_n = (cout + P.bn - 1) / P.bn; P.tiles_m = 1;
-    sg_deal(P, (size_t)G * K * M * (f32 ? 6 : 2));
     P.slices = (cin + 63) / 64; P.contraction = cin;
+    sg_deal(P, (size_t)G * K * M * (f32 ? 6 : 2), !f32);
     P.a_rows = N < TC_ROWS ? (N + 7) / 8 * 8 : TC_ROWS;
     P.rows_out = TC_ROWS; P.cols_out = cout;
     P.out = out; P.vec = (size_t)cout * elem_size(dtype) % 16 == 0;

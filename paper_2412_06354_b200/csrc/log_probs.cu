@@ -381,7 +381,7 @@ __device__ __forceinline__ float lp_chunk_max(uint4 v) {
 // equal scores, rows masked nearly throughout, scores that are not numbers) the classes are offered to a sorted list one by
 // one.  (Offered one by one always, 256 x 170,000 bf16, ten best: 175 us.)
 constexpr int LP_CAND = 256;
-constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory
+constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory (steps of four)
 
 template <typename T, int W>
 __global__ void __launch_bounds__(256)
@@ -433,50 +433,57 @@ log_probs_kernel(const LpParams P) {
     run.clear();
     const bool list = P.top > 0;
     constexpr int U = 4;  // chunks in flight per lane
-    int n = 0;
-    // chunks of the row alone: all but its two ends
+    // Chunks of the row alone are all but its two ends.  Four per step; the next four are on their way while these are added up; what
+    // lies behind the last counts as -inf.
     const int lo = first_class < 0 ? 1 : 0, hi = (int64_t)first_class + (int64_t)count * PER > P.C ? count - 1 : count;
-    for (int c = me; c - me < count; c += U * STEP) {  // the same for all lanes
-        uint4 v[U];
-        if (c >= lo && c + (U - 1) * STEP < hi) {  // four whole chunks: the maximum rises once at most
-            float cm[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = ld_16(zc + (int64_t)(c + u * STEP) * PER);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                cm[u] = lp_chunk_max<T>(v[u]);
-                if (list) sh_max[(n + u) * 256 + threadIdx.x] = cm[u];
-            }
-            const float bm = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
-            n += U;
-            if (bm > run.m) run.raise(bm);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float f[PER];
-                Chunk<T>::unpack(v[u], f);
-#pragma unroll
-                for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
-            }
-            continue;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c + u * STEP < count) v[u] = load(c + u * STEP);
+    const uint32_t nothing = PER == 8 ? 0xFF80FF80u : 0xFF800000u;
+    auto fetch = [&](int c, uint4* v) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (c + u * STEP >= count) break;
-            float f[PER];
-            scores(c + u * STEP, v[u], f);
-            float cm = f[0];
+            const int i = c + u * STEP;
+            v[u] = make_uint4(nothing, nothing, nothing, nothing);
+            if (i >= lo && i < hi) v[u] = ld_16(zc + (int64_t)i * PER);
+        }
+    };
+    int n = 0;
+    uint4 v[U];
+    fetch(me, v);
+    for (int c = me; c - me < count; c += U * STEP) {  // the same for all lanes
+        uint4 next[U];
+        fetch(c + U * STEP, next);
+        float cm[U];
 #pragma unroll
-            for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
-            if (list) sh_max[n * 256 + threadIdx.x] = cm;
-            ++n;
-            if (cm > run.m) run.raise(cm);
+        for (int u = 0; u < U; ++u) {
+            cm[u] = lp_chunk_max<T>(v[u]);
+            if (list) sh_max[(n + u) * 256 + threadIdx.x] = cm[u];
+        }
+        const float bm = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
+        n += U;
+        if (bm > run.m) run.raise(bm);  // the maximum rises once at most
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[PER];
+            Chunk<T>::unpack(v[u], f);
 #pragma unroll
             for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+            v[u] = next[u];
         }
     }
+    // the ends, each by the thread whose turn it would be
+    auto end = [&](int i) {
+        if (i % STEP != me) return;
+        float f[PER];
+        scores(i, load(i), f);
+        float cm = f[0];
+#pragma unroll
+        for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
+        if (list) sh_max[i / STEP * 256 + threadIdx.x] = cm;
+        if (cm > run.m) run.raise(cm);
+#pragma unroll
+        for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+    };
+    if (lo == 1 && count > 0) end(0);
+    if (hi < count && count - 1 >= lo) end(count - 1);
     const float mine = run.m;  // its own largest score
     LpStats st = run.stats();
     lp_join_lanes(st, lane);
@@ -557,9 +564,9 @@ log_probs_kernel(const LpParams P) {
             __syncthreads();
             floor = sh_floor;
         }
-        for (int k = 0; k < n; ++k) {
-            if (!(sh_max[k * 256 + threadIdx.x] >= floor)) continue;
+        for (int k = 0; k < n && mine >= floor; ++k) {
             const int i = k * STEP + me;
+            if (!(sh_max[k * 256 + threadIdx.x] >= floor) || i >= count) continue;
             float f[PER];
             Chunk<T>::unpack(load(i), f);
 #pragma unroll
@@ -839,13 +846,13 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
         else C <= 16 ? run(log_probs_few_kernel<__nv_bfloat16, 2>) : C <= 32 ? run(log_probs_few_kernel<__nv_bfloat16, 4>) : C <= 48 ? run(log_probs_few_kernel<__nv_bfloat16, 6>) : run(log_probs_few_kernel<__nv_bfloat16, 8>);
     } else if (C <= LP_WARP_CLASSES) {
         const dim3 grid((unsigned)ceil_div(N, 8));
-        const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32) * 1024 : 0;
+        const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32 * 4) * 4096 : 0;
         if (f32) launch_overlapped(log_probs_kernel<float, 1>, grid, dim3(256), smem, st, P);
         else launch_overlapped(log_probs_kernel<__nv_bfloat16, 1>, grid, dim3(256), smem, st, P);
     } else {
         const int64_t blocks = (int64_t)N * lw.parts;
         GNN_REQUIRE(blocks <= INT32_MAX, GNN_ERR_UNSUPPORTED, "%s: too many rows", who);
-        const size_t smem = top > 0 ? (size_t)ceil_div(ceil_div(chunks, lw.parts), 256) * 1024 : 0;
+        const size_t smem = top > 0 ? (size_t)ceil_div(ceil_div(chunks, lw.parts), 256 * 4) * 4096 : 0;
         const gnn_status rc = f32 ? allow_big_smem(who, (const void*)log_probs_kernel<float, 8>, LP_SLOT, LP_CHUNKS * 1024)
                                   : allow_big_smem(who, (const void*)log_probs_kernel<__nv_bfloat16, 8>, LP_SLOT + 1, LP_CHUNKS * 1024);
         if (rc != GNN_OK) return rc;

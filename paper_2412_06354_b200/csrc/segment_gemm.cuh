@@ -19,6 +19,9 @@
 //               170,000 x 128 -> 128, 1334 tiles dealt out to 148 SMs one by one: a tenth round for a few.
 //   otherwise:  tiles of 128 rows dealt out, all columns of a tile side by side: neighbouring CTAs share a segment's weights in L2, which
 //               could not hold all segments' at once; and where there are few rows.
+//   pair:       such a tile is 256 rows, a slice of weights serves both halves, one accumulator each.  An SM takes about 60 bytes a
+//               cycle from L2: 48 KB a slice of 128 x 256 are 820 cycles of copies beside 512 of products, 64 KB of 256 x 256 are 1090
+//               beside 1024.  The epilogue no longer runs beside the next tile's products, which long contractions make up for.
 // SG_DW: the rows are cut into equal parts, whatever the segments; a CTA takes one block [128 features x bn columns] of the
 // result over one part and finishes it for each segment that it meets there.  A segment that lies in one part is written at
 // once; one that is cut leaves an fp32 partial per part (two per part at most: the segment cut at its start, the one cut at
@@ -61,6 +64,7 @@ struct SegGemmParams {
     int64_t N;
     int64_t units;           // tiles, or ranges x blocks of columns (SG_DW: parts x blocks of the result)
     int ranges, resident;    // see above
+    int pair;                // tiles of 256 rows: both accumulators at once
     unsigned per_range, longer;
     int slices, contraction; // (not SG_DW) slices of the contraction, its elements
     int tiles_n, tiles_m;    // blocks of output columns; of features (SG_DW)
@@ -217,15 +221,22 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
             }
         }
     } else if constexpr (MODE != SG_DW) {
-        // unit = number of a tile of 128 rows * tiles_n + block of columns
+        // unit = number of a tile of 128 (pair: 256) rows * tiles_n + block of columns
         const unsigned nn = (unsigned)P.tiles_n, ds = gridDim.x / nn, dn = gridDim.x % nn;
         unsigned n = blockIdx.x % nn;
         int64_t s = blockIdx.x / nn;
         SegCursor<7> at;
+        SegCursor<8> at2;
         for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
-            const int64_t lo = at.at(P, s);
-            const SegRows t = {lo, lo + TC_ROWS < at.b ? lo + TC_ROWS : at.b, at.g, at.a, at.b};
-            if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            if (P.pair) {
+                const int64_t lo = at2.at(P, s);
+                const SegRows t = {lo, lo + 2 * TC_ROWS < at2.b ? lo + 2 * TC_ROWS : at2.b, at2.g, at2.a, at2.b};
+                if (at2.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            } else {
+                const int64_t lo = at.at(P, s);
+                const SegRows t = {lo, lo + TC_ROWS < at.b ? lo + TC_ROWS : at.b, at.g, at.a, at.b};
+                if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            }
             s += ds;
             n += dn;
             if (n >= nn) { n -= nn; ++s; }
@@ -345,7 +356,8 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     }
     const uint32_t b_bytes = (uint32_t)bn * 128u;
     const int nres = P.resident;  // (SG_DW: 0)
-    const uint32_t slot_bytes = SG_A_BYTES + (nres ? 0u : b_bytes), b_tile = (uint32_t)P.slices * b_bytes;
+    const bool pair = MODE != SG_DW && P.pair != 0;
+    const uint32_t a_bytes = pair ? 2 * SG_A_BYTES : SG_A_BYTES, slot_bytes = a_bytes + (nres ? 0u : b_bytes), b_tile = (uint32_t)P.slices * b_bytes;
     const uint32_t stage0 = base, res0 = base + SG_EPI_WARPS * SG_STAGING, ring0 = res0 + (uint32_t)nres * b_tile;
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
@@ -404,8 +416,9 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             for (int j = 0; j < slices; ++j, ring.next()) {
                 const int s = (int)ring.s;
                 if (!sg_wait(empty(s), ring.parity ^ 1u)) { failed = true; return false; }
-                sg_expect(full(s), nres ? a_box : a_box + b_bytes);
-                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + SG_A_BYTES;
+                const bool both = pair && t.hi - t.lo > TC_ROWS;
+                sg_expect(full(s), (both ? 2 * a_box : a_box) + (nres ? 0u : b_bytes));
+                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = a0 + a_bytes;
                 if constexpr (MODE == SG_DW) {
                     const int row = (int)(t.lo + (int64_t)j * 64);
 #pragma unroll
@@ -415,6 +428,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         if (h * 64 < bn) sg_load(b0 + (uint32_t)h * 8192u, &mapB, nb * bn + h * 64, row, 0, full(s), once);
                 } else {
                     sg_load(a0, &mapA, j * STEP, (int)t.lo, 0, full(s), once);
+                    if (both) sg_load(a0 + SG_A_BYTES, &mapA, j * STEP, (int)t.lo + TC_ROWS, 0, full(s), once);
                     if (!nres) load_b(b0, j, t.g, nb, full(s));
                 }
             }
@@ -428,7 +442,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     } else if (warp == 1) {
         const uint32_t idesc = MODE == SG_I8 ? make_idesc_i8(bn) : make_idesc(bn, MODE != SG_DX, MODE == SG_DW);
         SgRing ring(S), sets(nres ? nres : 1);
-        uint32_t lt = 0, res = 0, last_set = 0;
+        uint32_t lt = 0, second = 0, res = 0, last_set = 0;  // tiles; tiles with a second half
         int held_g = -1, held_n = -1;
         walk([&](const SegRows& t, int, int nb, int64_t) {
             if (nres && (t.g != held_g || nb != held_n)) {
@@ -440,13 +454,14 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                 held_g = t.g;
                 held_n = nb;
             }
-            const uint32_t a = lt & 1u;
+            const bool both = pair && t.hi - t.lo > TC_ROWS;
+            const uint32_t a = pair ? 0u : lt & 1u;
             const uint32_t dacc = tmem_base + a * acc_cols;
             const int slices = slices_of(t);
-            if (!sg_wait(acc_empty(a), ((lt >> 1) & 1u) ^ 1u)) { failed = true; return false; }
+            if (!sg_wait(acc_empty(a), ((pair ? lt : lt >> 1) & 1u) ^ 1u) || (both && !sg_wait(acc_empty(1), (second & 1u) ^ 1u))) { failed = true; return false; }
             for (int j = 0; j < slices; ++j, ring.next()) {
                 const int s = (int)ring.s;
-                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = nres ? res + (uint32_t)j * b_bytes : a0 + SG_A_BYTES;
+                const uint32_t a0 = ring0 + (uint32_t)s * slot_bytes, b0 = nres ? res + (uint32_t)j * b_bytes : a0 + a_bytes;
                 if (!sg_wait(full(s), ring.parity)) { failed = true; return false; }
                 if constexpr (MODE == SG_DW) {
                     const int have = (int)(t.hi - t.lo - (int64_t)j * 64);
@@ -471,9 +486,22 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     if constexpr (MODE == SG_I8) sg_mma_i8(dacc, da, db, idesc, more);
                     else sg_mma_bf16(dacc, da, db, idesc, more);
                 }
+                if (MODE != SG_DW && both) {
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const uint64_t da = ad + (uint64_t)(SG_A_BYTES / 16 + kk * 2), db = bd + (uint64_t)(kk * (B_MN ? 128 : 2));
+                        const uint32_t more = kk > 0 ? 1u : j > 0;
+                        if constexpr (MODE == SG_I8) sg_mma_i8(dacc + acc_cols, da, db, idesc, more);
+                        else sg_mma_bf16(dacc + acc_cols, da, db, idesc, more);
+                    }
+                }
                 sg_commit(empty(s));
             }
             sg_commit(acc_full(a));
+            if (both) {
+                sg_commit(acc_full(1));
+                ++second;
+            }
             ++lt;
             return true;
         });
@@ -482,10 +510,9 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     } else {
         const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
-        uint32_t lt = 0;
+        uint32_t lt = 0, second = 0;
         int staged_g = -1, staged_n = -1;
         walk([&](const SegRows& t, int mb, int nb, int64_t part) {
-            const uint32_t a = lt & 1u;
             if ((MODE == SG_Y || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
                 asm volatile("bar.sync 1, 512;" ::: "memory");
@@ -497,78 +524,84 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                 staged_g = t.g;
                 staged_n = nb;
             }
-            if (!sg_wait(acc_full(a), (lt >> 1) & 1u)) { failed = true; return false; }
-            tc_fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
-            const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - t.lo - quarter * 32;
-            const int rows = (int)(left < 32 ? left : 32);
-            const bool cut = MODE == SG_DW && (t.a != t.lo || t.b != t.hi);
-            const int c_base = nb * bn, c_end = P.cols_out;
-            float sx = 0.f;
-            if (MODE == SG_I8 && lane < rows) sx = P.sx[t.lo + quarter * 32 + lane];
-            // four sums at column c of the tile -> values before relu
-            auto finish4 = [&](int c, const uint32_t* r, float* f) {
-                if constexpr (MODE == SG_I8) {
-                    const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c]), b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
-                    const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) f[q] = fmaf(f[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
-                } else if constexpr (MODE == SG_Y) {
-                    const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
-                    f[0] = __uint_as_float(r[0]) + b.x; f[1] = __uint_as_float(r[1]) + b.y; f[2] = __uint_as_float(r[2]) + b.z; f[3] = __uint_as_float(r[3]) + b.w;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(r[q]);
-                }
-            };
-            auto send = [&](auto* out, int64_t ld, bool vec, auto with_relu) {
-                using O = typename std::remove_pointer<decltype(out)>::type;
-                constexpr int WIDE = 64 / sizeof(O), PER = Chunk<O>::N;  // columns of a staging row: 16 or 32; of a chunk
-                for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
-                    if (c_base + cb * WIDE >= c_end || rows <= 0) break;  // the whole warp
-                    uint32_t r[WIDE];
-#pragma unroll
-                    for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
-                    tmem_ld_wait();
-                    float f[WIDE];
+            const int halves = pair && t.hi - t.lo > TC_ROWS ? 2 : 1;
+            for (int half = 0; half < halves; ++half) {
+                const uint32_t a = pair ? (uint32_t)half : lt & 1u;
+                if (!sg_wait(acc_full(a), (half ? second : pair ? lt : lt >> 1) & 1u)) { failed = true; return false; }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
+                const int64_t row0 = t.lo + half * TC_ROWS + quarter * 32;  // (not SG_DW)
+                const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - row0;
+                const int rows = (int)(left < 32 ? left : 32);
+                const bool cut = MODE == SG_DW && (t.a != t.lo || t.b != t.hi);
+                const int c_base = nb * bn, c_end = P.cols_out;
+                float sx = 0.f;
+                if (MODE == SG_I8 && lane < rows) sx = P.sx[row0 + lane];
+                // four sums at column c of the tile -> values before relu
+                auto finish4 = [&](int c, const uint32_t* r, float* f) {
                     if constexpr (MODE == SG_I8) {
-                        if (P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
+                        const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c]), b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
+                        const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                            for (int q = 0; q < WIDE; ++q) f[q] = __uint_as_float(r[q] + 0x4B400000u) - 12582912.f;
-                        } else {
+                        for (int q = 0; q < 4; ++q) f[q] = fmaf(f[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
+                    } else if constexpr (MODE == SG_Y) {
+                        const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
+                        f[0] = __uint_as_float(r[0]) + b.x; f[1] = __uint_as_float(r[1]) + b.y; f[2] = __uint_as_float(r[2]) + b.z; f[3] = __uint_as_float(r[3]) + b.w;
+                    } else {
 #pragma unroll
-                            for (int q = 0; q < WIDE; ++q) f[q] = sg_int_float((int)r[q], q & 1);
+                        for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(r[q]);
+                    }
+                };
+                auto send = [&](auto* out, int64_t ld, bool vec, auto with_relu) {
+                    using O = typename std::remove_pointer<decltype(out)>::type;
+                    constexpr int WIDE = 64 / sizeof(O), PER = Chunk<O>::N;  // columns of a staging row: 16 or 32; of a chunk
+                    for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
+                        if (c_base + cb * WIDE >= c_end || rows <= 0) break;  // the whole warp
+                        uint32_t r[WIDE];
+#pragma unroll
+                        for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
+                        tmem_ld_wait();
+                        float f[WIDE];
+                        if constexpr (MODE == SG_I8) {
+                            if (P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
+#pragma unroll
+                                for (int q = 0; q < WIDE; ++q) f[q] = __uint_as_float(r[q] + 0x4B400000u) - 12582912.f;
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < WIDE; ++q) f[q] = sg_int_float((int)r[q], q & 1);
+                            }
                         }
-                    }
-                    __syncwarp();
+                        __syncwarp();
 #pragma unroll
-                    for (int q = 0; q < WIDE / PER; ++q) {
+                        for (int q = 0; q < WIDE / PER; ++q) {
 #pragma unroll
-                        for (int k = 0; k < PER; k += 4) finish4(cb * WIDE + q * PER + k, r + q * PER + k, f + q * PER + k);
-                        sg_stage(stg, lane, q, sg_pack<decltype(with_relu)::value>((O*)nullptr, f + q * PER));
+                            for (int k = 0; k < PER; k += 4) finish4(cb * WIDE + q * PER + k, r + q * PER + k, f + q * PER + k);
+                            sg_stage(stg, lane, q, sg_pack<decltype(with_relu)::value>((O*)nullptr, f + q * PER));
+                        }
+                        __syncwarp();
+                        sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
                     }
-                    __syncwarp();
-                    sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
-                }
-            };
-            if constexpr (MODE == SG_DW) {
-                const int64_t off = (int64_t)(mb * 128 + quarter * 32) * P.cols_out;
-                const int64_t size = (int64_t)P.rows_out * P.cols_out;
-                if (cut) {
-                    // cut at the part's start: partial 2p, else (at its end) 2p + 1
-                    const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
-                    send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0, std::false_type());
+                };
+                if constexpr (MODE == SG_DW) {
+                    const int64_t off = (int64_t)(mb * 128 + quarter * 32) * P.cols_out;
+                    const int64_t size = (int64_t)P.rows_out * P.cols_out;
+                    if (cut) {
+                        // cut at the part's start: partial 2p, else (at its end) 2p + 1
+                        const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
+                        send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0, std::false_type());
+                    } else {
+                        send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0, std::false_type());
+                    }
                 } else {
-                    send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0, std::false_type());
+                    T* const to = (T*)P.out + row0 * P.cols_out;
+                    if (MODE != SG_DX && P.relu) send(to, P.cols_out, P.vec != 0, std::true_type());
+                    else send(to, P.cols_out, P.vec != 0, std::false_type());
                 }
-            } else {
-                T* const to = (T*)P.out + (t.lo + quarter * 32) * P.cols_out;
-                if (MODE != SG_DX && P.relu) send(to, P.cols_out, P.vec != 0, std::true_type());
-                else send(to, P.cols_out, P.vec != 0, std::false_type());
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty(a));
+                second += (uint32_t)half;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(acc_empty(a));
             ++lt;
             return true;
         });
@@ -597,12 +630,15 @@ inline int sg_block(int cols, int most, int64_t row_tiles) {
     return bn;
 }
 
-// How the tiles of SG_Y, SG_DX and SG_I8 are dealt out (see above): ranges where all weights together are a fraction of L2 and the rows
-// give every SM a few tiles.
-inline void sg_deal(SegGemmParams& P, size_t weight_bytes) {
+// How the tiles of SG_Y, SG_DX and SG_I8 are dealt out (see above).  Pairs: where the weights of a tile are too many to stay, contractions of
+// eight slices and a tile of 256 rows for every SM (65,536 x 1024 -> 1024 over 64 segments: XX us in ones, XX in pairs).
+// Otherwise ranges where all weights together are a fraction of L2 and the rows give every SM a few tiles.
+inline bool sg_stays(const SegGemmParams& P) { return SG_EPI_WARPS * SG_STAGING + (size_t)P.bn * 128 * P.slices + 4 * SG_A_BYTES <= SG_SMEM_MAX; }
+inline void sg_deal(SegGemmParams& P, size_t weight_bytes, bool pairs = true) {
     const int64_t row_tiles = P.N / TC_ROWS + P.G;
-    P.ranges = weight_bytes <= ((size_t)32 << 20) && P.N / TC_ROWS * P.tiles_n >= 296 && P.G <= P.N / 512 && P.tiles_n <= 148 ? 148 / P.tiles_n : 0;
-    P.units = (P.ranges ? P.ranges : row_tiles) * P.tiles_n;
+    P.pair = pairs && !sg_stays(P) && P.slices >= 8 && P.N / (2 * TC_ROWS) * P.tiles_n >= 148;
+    P.ranges = !P.pair && weight_bytes <= ((size_t)32 << 20) && P.N / TC_ROWS * P.tiles_n >= 296 && P.G <= P.N / 512 && P.tiles_n <= 148 ? 148 / P.tiles_n : 0;
+    P.units = (P.ranges ? P.ranges : P.pair ? P.N / (2 * TC_ROWS) + P.G : row_tiles) * P.tiles_n;
     if (P.ranges) {
         const int64_t blocks = (P.N >> 5) + P.G;
         P.per_range = (unsigned)(blocks / P.ranges);
@@ -618,7 +654,7 @@ static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA,
     const size_t fixed = SG_EPI_WARPS * SG_STAGING, b_bytes = (size_t)P.bn * 128, tile = MODE == SG_DW ? 0 : b_bytes * P.slices;
     // resident weights: two sets where they leave the ring eight slots, one where they leave it four
     P.resident = MODE != SG_DW && P.ranges > 0 ? (fixed + 2 * tile + 8 * SG_A_BYTES <= SG_SMEM_MAX ? 2 : fixed + tile + 4 * SG_A_BYTES <= SG_SMEM_MAX ? 1 : 0) : 0;
-    const size_t slot = SG_A_BYTES + (P.resident ? 0 : b_bytes), held = (size_t)P.resident * tile;
+    const size_t slot = (P.pair ? 2 : 1) * SG_A_BYTES + (P.resident ? 0 : b_bytes), held = (size_t)P.resident * tile;
     int stages = (int)((SG_SMEM_MAX - fixed - held) / slot);
     P.stages = stages > SG_MAX_STAGES ? SG_MAX_STAGES : stages;
     int cols = 32;

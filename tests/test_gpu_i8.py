@@ -94,7 +94,7 @@ def product_ref(q, sx, w, sw, b, relu):
 
 
 SHAPES = [(1, 1, 1), (1, 16, 8), (1, 1024, 1024), (3, 37, 5), (8, 48, 100), (9, 16, 8), (9, 1, 1), (17, 33, 3), (127, 128, 64), (128, 144, 65), (129, 256, 256), (300, 100, 47), (1000, 512, 328),
-          (64, 4096, 264), (700, 80, 1030), (20000, 64, 128), (2, 100, 70000 // 64)]
+          (64, 4096, 264), (700, 80, 1030), (20000, 64, 128), (2, 100, 70000 // 64), (40001, 1100, 300), (38100, 1024, 256), (40000, 256, 250)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

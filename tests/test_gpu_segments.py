@@ -281,3 +281,21 @@ def test_rows_by_consecutive_ranges(gnn, dtype, K, M):
     rX, SX, rW, SW = backward_ref(X, ptr, W, dY)
     close(dX, rX, SX, "dX")
     close(dW, rW, SW, "dW")
+
+
+@pytest.mark.parametrize("K,M", [(520, 200), (1030, 300)])
+def test_long_contractions_by_tiles_of_256_rows(gnn, K, M):
+    """Weights too many to stay in shared memory, rows enough for every SM: second halves of a tile full, cut, of one row, missing."""
+    import torch
+    sizes = [20000, 128, 129, 300, 1, 255, 256, 257, 0, 385, 18000]
+    X, ptr, W, b, dY = data("bf16", sizes, K, M, lead=3, tail=70, seed=K)
+    Xd, pd, Wd, bd, dYd = (t.cuda() for t in (X, ptr, W, b, dY))
+    Y, ws = gnn.linear_segments(Xd, pd, Wd, bias=bd, relu=True, return_ws=True)
+    assert status(ws) == 0
+    ref, S = forward_ref(X, ptr, W, b, True)
+    close(Y, ref, S, "relu(Y + b)")
+    Wt = W.transpose(1, 2).contiguous()  # dX with a contraction of K
+    dX, _, ws = gnn.linear_segments_backward(None, pd, Wt.cuda(), Xd, want_dW=False, return_ws=True)
+    assert status(ws) == 0
+    ref, S = forward_ref(X, ptr, W, None, False)
+    close(dX, ref, S, "dX")
