@@ -113,25 +113,24 @@ __device__ __forceinline__ SegFound last_segment(const SegGemmParams& P, F befor
         hi = min(hi, lo + step);
     }
 }
-// Block number s of 2^SHIFT rows -> its segment and first row, for ascending s: the segment of the last one is kept, so that most
+// Block number s of 2^shift rows -> its segment and first row, for ascending s: the segment of the last one is kept, so that most
 // are two comparisons and an addition.  (Searching anew for each, with 64-bit divisions, took the loader 1000 cycles a tile.)
-template <int SHIFT>
 struct SegCursor {
     int g;
     int64_t a, b, first, next;  // rows of segment g, its block numbers
     __device__ __forceinline__ SegCursor() : g(-1), a(0), b(0), first(0), next(0) {}
     // first row of block s; g < 0: before the first segment
-    __device__ __forceinline__ int64_t at(const SegGemmParams& P, int64_t s) {
+    __device__ __forceinline__ int64_t at(const SegGemmParams& P, int64_t s, int shift) {
         if (s >= next) {
-            const SegFound f = last_segment(P, [&](int q, int64_t v) { return (v >> SHIFT) + q <= s; });
+            const SegFound f = last_segment(P, [&](int q, int64_t v) { return (v >> shift) + q <= s; });
             if (f.g < 0) return 0;
             g = f.g;
             a = f.a;
             b = f.b;
-            first = (a >> SHIFT) + g;
-            next = (b >> SHIFT) + g + 1;  // (of the next segment; not above the true bound where seg_ptr descends)
+            first = (a >> shift) + g;
+            next = (b >> shift) + g + 1;  // (of the next segment; not above the true bound where seg_ptr descends)
         }
-        return a + ((s - first) << SHIFT);
+        return a + ((s - first) << shift);
     }
 };
 
@@ -206,9 +205,9 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
             const unsigned r = P.tiles_n == 1 ? u : u / (unsigned)P.tiles_n;
             const int n = (int)(u - r * (unsigned)P.tiles_n);
             const int64_t s0 = r * P.per_range + (r < P.longer ? r : P.longer), s1 = s0 + P.per_range + (r < P.longer ? 1u : 0u);
-            SegCursor<5> at;
+            SegCursor at;
             for (int64_t s = s0; s < s1;) {
-                const int64_t lo = at.at(P, s);
+                const int64_t lo = at.at(P, s, 5);
                 if (at.g < 0 || lo >= at.b) {  // rows of no segment before the first one, the empty block at a segment's end
                     s = at.g < 0 ? (seg_at(P, 0) >> 5) > s ? (seg_at(P, 0) >> 5) : s + 1 : at.next > s ? at.next : s + 1;
                     continue;
@@ -225,18 +224,12 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
         const unsigned nn = (unsigned)P.tiles_n, ds = gridDim.x / nn, dn = gridDim.x % nn;
         unsigned n = blockIdx.x % nn;
         int64_t s = blockIdx.x / nn;
-        SegCursor<7> at;
-        SegCursor<8> at2;
+        const int shift = P.pair ? 8 : 7;
+        SegCursor at;
         for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
-            if (P.pair) {
-                const int64_t lo = at2.at(P, s);
-                const SegRows t = {lo, lo + 2 * TC_ROWS < at2.b ? lo + 2 * TC_ROWS : at2.b, at2.g, at2.a, at2.b};
-                if (at2.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
-            } else {
-                const int64_t lo = at.at(P, s);
-                const SegRows t = {lo, lo + TC_ROWS < at.b ? lo + TC_ROWS : at.b, at.g, at.a, at.b};
-                if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
-            }
+            const int64_t lo = at.at(P, s, shift), hi = lo + ((int64_t)1 << shift);
+            const SegRows t = {lo, hi < at.b ? hi : at.b, at.g, at.a, at.b};
+            if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
             s += ds;
             n += dn;
             if (n >= nn) { n -= nn; ++s; }
@@ -527,16 +520,16 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             const int halves = pair && t.hi - t.lo > TC_ROWS ? 2 : 1;
             for (int half = 0; half < halves; ++half) {
                 const uint32_t a = pair ? (uint32_t)half : lt & 1u;
-                if (!sg_wait(acc_full(a), (half ? second : pair ? lt : lt >> 1) & 1u)) { failed = true; return false; }
-                tc_fence_after();
-                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
                 const int64_t row0 = t.lo + half * TC_ROWS + quarter * 32;  // (not SG_DW)
                 const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - row0;
                 const int rows = (int)(left < 32 ? left : 32);
-                const bool cut = MODE == SG_DW && (t.a != t.lo || t.b != t.hi);
-                const int c_base = nb * bn, c_end = P.cols_out;
                 float sx = 0.f;
                 if (MODE == SG_I8 && lane < rows) sx = P.sx[row0 + lane];
+                if (!sg_wait(acc_full(a), (half ? second : pair ? lt : lt >> 1) & 1u)) { failed = true; return false; }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * acc_cols;
+                const bool cut = MODE == SG_DW && (t.a != t.lo || t.b != t.hi);
+                const int c_base = nb * bn, c_end = P.cols_out;
                 // four sums at column c of the tile -> values before relu
                 auto finish4 = [&](int c, const uint32_t* r, float* f) {
                     if constexpr (MODE == SG_I8) {
