@@ -305,31 +305,18 @@ __device__ __forceinline__ void sg_zero_outside(const SegGemmParams& P, T* out) 
     for (int64_t i = p1 + me; i < end; i += all) out[i] = T(0.f);
 }
 
-// int32 -> fp32, one rounding.  The conversion instruction runs at a quarter of the rate of additions: every other value goes by its
-// halves, each exact in fp32 (low 16 bits on top of 2^23, high ones on 1.5 * 2^23), joined by one fma.
-__device__ __forceinline__ float sg_int_float(int x, bool halves) {
-    if (!halves) return (float)x;
-    const float lo = __uint_as_float(0x4B000000u | ((uint32_t)x & 0xFFFFu)) - 8388608.f;
-    const float hi = __int_as_float(0x4B400000 + (x >> 16)) - 12582912.f;
-    return fmaf(hi, 65536.f, lo);
-}
-
-// a chunk of 16 bytes, max(., 0) with the rounding; a NaN stays
-template <bool RELU>
-__device__ __forceinline__ uint4 sg_pack(const float*, const float* f) {
+// a chunk of 16 bytes, not under floor: 0 (relu) or -inf, twice as bf16; a NaN stays.  (Of rounded values, as of the sums.)
+__device__ __forceinline__ uint4 sg_pack(const float* f, const float*, uint32_t floor) {
     float g[4] = {f[0], f[1], f[2], f[3]};
-    if (RELU) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(g[q]));
-    }
+    for (int q = 0; q < 4; ++q) asm("max.NaN.f32 %0, %0, %1;" : "+f"(g[q]) : "f"(__uint_as_float(floor & 0xFFFF0000u)));
     return Chunk<float>::pack(g);
 }
-template <bool RELU>
-__device__ __forceinline__ uint4 sg_pack(const __nv_bfloat16*, const float* f) {
-    if (!RELU) return Chunk<__nv_bfloat16>::pack(f);
-    uint32_t w[4];
+__device__ __forceinline__ uint4 sg_pack(const float* f, const __nv_bfloat16*, uint32_t floor) {
+    const uint4 v = Chunk<__nv_bfloat16>::pack(f);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(f[2 * q + 1]), "f"(f[2 * q]));
+    for (int q = 0; q < 4; ++q) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[q]) : "r"(floor));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -503,6 +490,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     } else {
         const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
+        const uint32_t floor = P.relu ? 0u : 0xFF80FF80u;
         uint32_t lt = 0, second = 0;
         int staged_g = -1, staged_n = -1;
         walk([&](const SegRows& t, int mb, int nb, int64_t part) {
@@ -536,7 +524,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c]), b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
                         const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) f[q] = fmaf(f[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
+                        for (int q = 0; q < 4; ++q) f[q] = fmaf((float)(int)r[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
                     } else if constexpr (MODE == SG_Y) {
                         const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
                         f[0] = __uint_as_float(r[0]) + b.x; f[1] = __uint_as_float(r[1]) + b.y; f[2] = __uint_as_float(r[2]) + b.z; f[3] = __uint_as_float(r[3]) + b.w;
@@ -545,7 +533,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(r[q]);
                     }
                 };
-                auto send = [&](auto* out, int64_t ld, bool vec, auto with_relu) {
+                auto send = [&](auto* out, int64_t ld, bool vec) {
                     using O = typename std::remove_pointer<decltype(out)>::type;
                     constexpr int WIDE = 64 / sizeof(O), PER = Chunk<O>::N;  // columns of a staging row: 16 or 32; of a chunk
                     for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
@@ -555,21 +543,12 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
                         tmem_ld_wait();
                         float f[WIDE];
-                        if constexpr (MODE == SG_I8) {
-                            if (P.contraction <= 256) {  // sums inside +-2^22: on top of 1.5 * 2^23 they are a number's last bits
-#pragma unroll
-                                for (int q = 0; q < WIDE; ++q) f[q] = __uint_as_float(r[q] + 0x4B400000u) - 12582912.f;
-                            } else {
-#pragma unroll
-                                for (int q = 0; q < WIDE; ++q) f[q] = sg_int_float((int)r[q], q & 1);
-                            }
-                        }
                         __syncwarp();
 #pragma unroll
                         for (int q = 0; q < WIDE / PER; ++q) {
 #pragma unroll
                             for (int k = 0; k < PER; k += 4) finish4(cb * WIDE + q * PER + k, r + q * PER + k, f + q * PER + k);
-                            sg_stage(stg, lane, q, sg_pack<decltype(with_relu)::value>((O*)nullptr, f + q * PER));
+                            sg_stage(stg, lane, q, MODE == SG_DW || MODE == SG_DX ? Chunk<O>::pack(f + q * PER) : sg_pack(f + q * PER, (O*)nullptr, floor));
                         }
                         __syncwarp();
                         sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
@@ -581,14 +560,12 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     if (cut) {
                         // cut at the part's start: partial 2p, else (at its end) 2p + 1
                         const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
-                        send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0, std::false_type());
+                        send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0);
                     } else {
-                        send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0, std::false_type());
+                        send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0);
                     }
                 } else {
-                    T* const to = (T*)P.out + row0 * P.cols_out;
-                    if (MODE != SG_DX && P.relu) send(to, P.cols_out, P.vec != 0, std::true_type());
-                    else send(to, P.cols_out, P.vec != 0, std::false_type());
+                    send((T*)P.out + row0 * P.cols_out, P.cols_out, P.vec != 0);
                 }
                 tc_fence_before();
                 __syncwarp();
