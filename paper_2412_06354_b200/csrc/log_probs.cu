@@ -9,13 +9,16 @@
 // with the smaller maximum, whose own maximum counts again: exp(m1 - m2) (s1 + 1).
 // The k best: keys of (score, lower index first) that are all different, sorted over the lanes of a warp; a chunk whose largest
 // score does not pass the worst of them is left alone.
+#include <cooperative_groups.h>
+
 #include "tc_common.cuh"
 
 namespace gnn {
 
 constexpr int LP_TOP = 32;            // classes listed at most: a lane each
 constexpr int LP_WARP_CLASSES = 1024;  // rows up to here by a warp
-constexpr int LP_SLOT = 56;           // of allow_big_smem: two of them
+constexpr int LP_SLOT = 56;           // of allow_big_smem: four of them
+constexpr int LP_CLUSTER = 8;         // parts of a row that a cluster of blocks joins; more leave theirs in the workspace
 
 __device__ __forceinline__ float lp_exp(float d) {  // exp of d <= 0: 2^(d log2 e); the error of the product reaches what is below e^-10 by 1e-6 of it
     float e;
@@ -381,9 +384,9 @@ __device__ __forceinline__ float lp_chunk_max(uint4 v) {
 // equal scores, rows masked nearly throughout, scores that are not numbers) the classes are offered to a sorted list one by
 // one.  (Offered one by one always, 256 x 170,000 bf16, ten best: 175 us.)
 constexpr int LP_CAND = 256;
-constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory (steps of four)
+constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory
 
-template <typename T, int W>
+template <typename T, int W, bool CLUSTER>
 __global__ void __launch_bounds__(256)
 log_probs_kernel(const LpParams P) {
     pdl_wait();
@@ -433,57 +436,50 @@ log_probs_kernel(const LpParams P) {
     run.clear();
     const bool list = P.top > 0;
     constexpr int U = 4;  // chunks in flight per lane
-    // Chunks of the row alone are all but its two ends.  Four per step; the next four are on their way while these are added up; what
-    // lies behind the last counts as -inf.
-    const int lo = first_class < 0 ? 1 : 0, hi = (int64_t)first_class + (int64_t)count * PER > P.C ? count - 1 : count;
-    const uint32_t nothing = PER == 8 ? 0xFF80FF80u : 0xFF800000u;
-    auto fetch = [&](int c, uint4* v) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = c + u * STEP;
-            v[u] = make_uint4(nothing, nothing, nothing, nothing);
-            if (i >= lo && i < hi) v[u] = ld_16(zc + (int64_t)i * PER);
-        }
-    };
     int n = 0;
-    uint4 v[U];
-    fetch(me, v);
+    // chunks of the row alone: all but its two ends
+    const int lo = first_class < 0 ? 1 : 0, hi = (int64_t)first_class + (int64_t)count * PER > P.C ? count - 1 : count;
     for (int c = me; c - me < count; c += U * STEP) {  // the same for all lanes
-        uint4 next[U];
-        fetch(c + U * STEP, next);
-        float cm[U];
+        uint4 v[U];
+        if (c >= lo && c + (U - 1) * STEP < hi) {  // four whole chunks: the maximum rises once at most
+            float cm[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            cm[u] = lp_chunk_max<T>(v[u]);
-            if (list) sh_max[(n + u) * 256 + threadIdx.x] = cm[u];
+            for (int u = 0; u < U; ++u) v[u] = ld_16(zc + (int64_t)(c + u * STEP) * PER);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                cm[u] = lp_chunk_max<T>(v[u]);
+                if (list) sh_max[(n + u) * 256 + threadIdx.x] = cm[u];
+            }
+            const float bm = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
+            n += U;
+            if (bm > run.m) run.raise(bm);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[PER];
+                Chunk<T>::unpack(v[u], f);
+#pragma unroll
+                for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+            }
+            continue;
         }
-        const float bm = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
-        n += U;
-        if (bm > run.m) run.raise(bm);  // the maximum rises once at most
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c + u * STEP < count) v[u] = load(c + u * STEP);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (c + u * STEP >= count) break;
             float f[PER];
-            Chunk<T>::unpack(v[u], f);
+            scores(c + u * STEP, v[u], f);
+            float cm = f[0];
+#pragma unroll
+            for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
+            if (list) sh_max[n * 256 + threadIdx.x] = cm;
+            ++n;
+            if (cm > run.m) run.raise(cm);
 #pragma unroll
             for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
-            v[u] = next[u];
         }
     }
-    // the ends, each by the thread whose turn it would be
-    auto end = [&](int i) {
-        if (i % STEP != me) return;
-        float f[PER];
-        scores(i, load(i), f);
-        float cm = f[0];
-#pragma unroll
-        for (int k = 1; k < PER; ++k) cm = fmaxf(cm, f[k]);
-        if (list) sh_max[i / STEP * 256 + threadIdx.x] = cm;
-        if (cm > run.m) run.raise(cm);
-#pragma unroll
-        for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
-    };
-    if (lo == 1 && count > 0) end(0);
-    if (hi < count && count - 1 >= lo) end(count - 1);
     const float mine = run.m;  // its own largest score
     LpStats st = run.stats();
     lp_join_lanes(st, lane);
@@ -565,8 +561,8 @@ log_probs_kernel(const LpParams P) {
             floor = sh_floor;
         }
         for (int k = 0; k < n && mine >= floor; ++k) {
+            if (!(sh_max[k * 256 + threadIdx.x] >= floor)) continue;
             const int i = k * STEP + me;
-            if (!(sh_max[k * 256 + threadIdx.x] >= floor) || i >= count) continue;
             float f[PER];
             Chunk<T>::unpack(load(i), f);
 #pragma unroll
@@ -599,7 +595,26 @@ log_probs_kernel(const LpParams P) {
             }
         }
     }
-    if constexpr (W > 1) {
+    if constexpr (CLUSTER) {  // the parts of a row are the blocks of a cluster: the first one joins them
+        namespace cg = cooperative_groups;
+        cg::cluster_group all_parts = cg::this_cluster();
+        __shared__ LpStats sh_part;  // (not sh_stats, which other warps may still read)
+        __shared__ uint64_t sh_part_keys[LP_TOP];
+        if (warp == 0) {
+            if (lane == 0) sh_part = st;
+            sh_part_keys[lane] = best;
+        }
+        all_parts.sync();
+        if (part == 0 && warp == 0) {
+            st.clear();
+            if (lane < P.parts) st = *all_parts.map_shared_rank(&sh_part, lane);
+            lp_join_lanes(st, lane);
+            if (list)
+                for (int p = 1; p < P.parts; ++p) best = lp_merge(best, *all_parts.map_shared_rank(&sh_part_keys[lane], p), lane);
+        }
+        all_parts.sync();  // nobody leaves while it is read
+        if (part != 0 || warp != 0) return;
+    } else if constexpr (W > 1) {
         if (warp != 0) return;
         if (P.parts > 1) {
             const int64_t at = row * P.parts + part;
@@ -797,13 +812,32 @@ static int64_t lp_parts(int64_t N, int64_t C, int s) {
 // a thread per row: few classes, and rows enough to fill the SMs with threads
 static bool lp_few(int64_t N, int C, int top) { return C <= LP_FEW && N >= 4096; }
 
+// launch_overlapped with clusters
+template <class... Params, class... Args>
+static void launch_cluster(void (*kernel)(Params...), unsigned blocks, unsigned size, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = size;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);  // errors: GNN_CHECK_LAUNCH of the caller
+}
+
 struct LpWs {
     int64_t parts;
     size_t keys, bytes;
     LpWs(int64_t N, int C, int top, gnn_dtype dtype) {
         parts = N > 0 && C > LP_WARP_CLASSES ? lp_parts(N, C, elem_size(dtype)) : 1;
-        keys = parts > 1 ? up256((size_t)N * parts * 16) : 0;
-        bytes = keys + (parts > 1 ? up256((size_t)N * parts * top * 8) : 0);
+        keys = parts > LP_CLUSTER ? up256((size_t)N * parts * 16) : 0;
+        bytes = keys + (parts > LP_CLUSTER ? up256((size_t)N * parts * top * 8) : 0);
     }
 };
 
@@ -846,19 +880,25 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
         else C <= 16 ? run(log_probs_few_kernel<__nv_bfloat16, 2>) : C <= 32 ? run(log_probs_few_kernel<__nv_bfloat16, 4>) : C <= 48 ? run(log_probs_few_kernel<__nv_bfloat16, 6>) : run(log_probs_few_kernel<__nv_bfloat16, 8>);
     } else if (C <= LP_WARP_CLASSES) {
         const dim3 grid((unsigned)ceil_div(N, 8));
-        const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32 * 4) * 4096 : 0;
-        if (f32) launch_overlapped(log_probs_kernel<float, 1>, grid, dim3(256), smem, st, P);
-        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 1>, grid, dim3(256), smem, st, P);
+        const size_t smem = top > 0 ? (size_t)ceil_div(chunks, 32) * 1024 : 0;
+        if (f32) launch_overlapped(log_probs_kernel<float, 1, false>, grid, dim3(256), smem, st, P);
+        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 1, false>, grid, dim3(256), smem, st, P);
     } else {
         const int64_t blocks = (int64_t)N * lw.parts;
         GNN_REQUIRE(blocks <= INT32_MAX, GNN_ERR_UNSUPPORTED, "%s: too many rows", who);
-        const size_t smem = top > 0 ? (size_t)ceil_div(ceil_div(chunks, lw.parts), 256 * 4) * 4096 : 0;
-        const gnn_status rc = f32 ? allow_big_smem(who, (const void*)log_probs_kernel<float, 8>, LP_SLOT, LP_CHUNKS * 1024)
-                                  : allow_big_smem(who, (const void*)log_probs_kernel<__nv_bfloat16, 8>, LP_SLOT + 1, LP_CHUNKS * 1024);
+        const size_t smem = top > 0 ? (size_t)ceil_div(ceil_div(chunks, lw.parts), 256) * 1024 : 0;
+        const bool cluster = lw.parts > 1 && lw.parts <= LP_CLUSTER;
+        auto run = [&](auto kernel, int slot) {
+            const gnn_status rc = allow_big_smem(who, (const void*)kernel, slot, LP_CHUNKS * 1024);
+            if (rc != GNN_OK) return rc;
+            if (cluster) launch_cluster(kernel, (unsigned)blocks, (unsigned)lw.parts, smem, st, P);
+            else launch_overlapped(kernel, dim3((unsigned)blocks), dim3(256), smem, st, P);
+            return GNN_OK;
+        };
+        const gnn_status rc = f32 ? cluster ? run(log_probs_kernel<float, 8, true>, LP_SLOT) : run(log_probs_kernel<float, 8, false>, LP_SLOT + 1)
+                                  : cluster ? run(log_probs_kernel<__nv_bfloat16, 8, true>, LP_SLOT + 2) : run(log_probs_kernel<__nv_bfloat16, 8, false>, LP_SLOT + 3);
         if (rc != GNN_OK) return rc;
-        if (f32) launch_overlapped(log_probs_kernel<float, 8>, dim3((unsigned)blocks), dim3(256), smem, st, P);
-        else launch_overlapped(log_probs_kernel<__nv_bfloat16, 8>, dim3((unsigned)blocks), dim3(256), smem, st, P);
-        if (lw.parts > 1) {
+        if (lw.parts > LP_CLUSTER) {
             const dim3 grid((unsigned)N);
             if (f32) launch_overlapped(log_probs_join_kernel<float>, grid, dim3(256), 0, st, P);
             else launch_overlapped(log_probs_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, P);
