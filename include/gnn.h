@@ -505,7 +505,8 @@ gnn_status gnn_linear_backward(const void* X, const void* W, const void* dY, int
  * from seg_ptr[G] on) become 0.  X [N,K], W [G,K,M], Y [N,M] of dtype, bias float [G,M] or NULL; relu != 0: max(., 0)
  * before the single rounding (a NaN stays).  K and M: any up to 8192 (fp32: 2048; GNN_ERR_UNSUPPORTED beyond), G K < 2^31.
  * Matrices and ws are 16-byte aligned.  Tensor cores with fp32 accumulation: bf16 directly, fp32 by an exact three-term bf16
- * split as in gnn_linear (a value that is not finite gives NaN in the results it enters).
+ * split as in gnn_linear (a value that is not finite, or whose magnitude is above 3.38e38, gives NaN in the results it enters).
+ * A seg_ptr that descends gives unspecified results; every access stays inside the arguments.
  * Rows of one segment only ever meet their own weight: what another segment holds (infinities, NaN) does not reach them.
  * ws: gnn_linear_segments_workspace(..., backward = 0) bytes, asked for the sizes of each call; it holds copies of bf16
  * matrices whose rows do not start on 16 bytes and the terms of fp32 ones.  Its first 4 bytes are the status word of

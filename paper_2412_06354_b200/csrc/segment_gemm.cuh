@@ -84,7 +84,7 @@ struct SegGemmParams {
     int reset;
 };
 
-// rows [lo, hi) of segment g, kept inside [0, N) whatever seg_ptr holds
+// rows [lo, hi) of segment g, kept inside [0, N) and behind a whatever seg_ptr holds
 struct SegRows { int64_t lo, hi; int g; int64_t a, b; };  // a, b: all rows of the segment
 __device__ __forceinline__ int64_t seg_at(const SegGemmParams& P, int g) {
     if (!P.seg_ptr) return g > 0 ? P.N : 0;
@@ -208,7 +208,7 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
             SegCursor at;
             for (int64_t s = s0; s < s1;) {
                 const int64_t lo = at.at(P, s, 5);
-                if (at.g < 0 || lo >= at.b) {  // rows of no segment before the first one, the empty block at a segment's end
+                if (at.g < 0 || lo < at.a || lo >= at.b) {  // rows of no segment before the first one, the empty block at a segment's end (lo < a: seg_ptr descends)
                     s = at.g < 0 ? (seg_at(P, 0) >> 5) > s ? (seg_at(P, 0) >> 5) : s + 1 : at.next > s ? at.next : s + 1;
                     continue;
                 }
@@ -229,7 +229,7 @@ __device__ __forceinline__ void sg_walk(const SegGemmParams& P, Body body) {
         for (int64_t u = blockIdx.x; u < P.units; u += gridDim.x) {
             const int64_t lo = at.at(P, s, shift), hi = lo + ((int64_t)1 << shift);
             const SegRows t = {lo, hi < at.b ? hi : at.b, at.g, at.a, at.b};
-            if (at.g >= 0 && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;
+            if (at.g >= 0 && t.lo >= at.a && t.hi > t.lo && !body(t, 0, (int)n, (int64_t)0)) return;  // (lo < a: seg_ptr descends)
             s += ds;
             n += dn;
             if (n >= nn) { n -= nn; ++s; }
