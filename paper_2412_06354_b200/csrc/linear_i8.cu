@@ -354,7 +354,7 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     CUtensorMap mapA, mapB;
     if (!make_map_planes(&mapA, xp, 1, 1, N, K, up16(K), P.a_rows) || !make_map_planes(&mapB, wp, 1, 1, M, K, up16(K), P.bn))
         GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-    return dtype == GNN_F32 ? sg_launch<SG_I8, float>(who, I8_SLOT, mapA, mapB, P, st) : sg_launch<SG_I8, __nv_bfloat16>(who, I8_SLOT + 1, mapA, mapB, P, st);
+    return dtype == GNN_F32 ? sg_launch<SG_I8, float>(who, I8_SLOT, mapA, mapB, P, 0, st) : sg_launch<SG_I8, __nv_bfloat16>(who, I8_SLOT + 1, mapA, mapB, P, 0, st);
 }
 
 }  // extern "C"

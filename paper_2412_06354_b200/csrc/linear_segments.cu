@@ -206,8 +206,8 @@ static gnn_status seg_rows(const char* who, bool dx, const void* in, const void*
     if (!make_map_planes(&mapA, in, f32 ? 2 : 0, 1, N, cin, apart(cin, dtype), P.a_rows) ||
         !make_map_planes(&mapB, w, 0, (int64_t)(f32 ? 3 : 1) * G, K, M, up8(M), dx ? P.bn : 64))
         GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-    if (f32) return segment_gemm_f32(who, dx ? SG_DX : SG_Y, LS_SLOT + dx, mapA, mapB, P, st);
-    return dx ? sg_launch<SG_DX, __nv_bfloat16>(who, LS_SLOT + 2, mapA, mapB, P, st) : sg_launch<SG_Y, __nv_bfloat16>(who, LS_SLOT + 3, mapA, mapB, P, st);
+    if (f32) return segment_gemm_f32(who, dx ? SG_DX : SG_Y, LS_SLOT + dx, mapA, mapB, P, 0, st);
+    return dx ? sg_launch<SG_DX, __nv_bfloat16>(who, LS_SLOT + 2, mapA, mapB, P, 0, st) : sg_launch<SG_Y, __nv_bfloat16>(who, LS_SLOT + 3, mapA, mapB, P, 0, st);
 }
 
 static gnn_status zero(const char* who, void* p, size_t bytes, cudaStream_t st) {
@@ -300,7 +300,9 @@ gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, c
         const int type = f32 ? 2 : 0, box_rows = f32 ? 32 : 64;
         if (!make_map_planes(&mapA, Xp, type, 1, N, K, apart(K, dtype), box_rows) || !make_map_planes(&mapB, dYp, type, 1, N, M, apart(M, dtype), box_rows))
             GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
-        const gnn_status rc = f32 ? segment_gemm_f32(who, SG_DW, LS_SLOT + 4, mapA, mapB, P, st) : sg_launch<SG_DW, __nv_bfloat16>(who, LS_SLOT + 5, mapA, mapB, P, st);
+        const int64_t part_rows_all = sw.parts > 1 ? 2 * sw.parts * K : 1;  // (one part: no partials)
+        const gnn_status rc = f32 ? segment_gemm_f32(who, SG_DW, LS_SLOT + 4, mapA, mapB, P, part_rows_all, st)
+                                  : sg_launch<SG_DW, __nv_bfloat16>(who, LS_SLOT + 5, mapA, mapB, P, part_rows_all, st);
         if (rc != GNN_OK) return rc;
         const int64_t size = (int64_t)K * M;
         auto sum = [&](auto kernel, auto* to, int elements) {

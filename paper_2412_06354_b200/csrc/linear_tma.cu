@@ -296,19 +296,23 @@ static bool make_map_ld(CUtensorMap* m, const void* ptr, int64_t rows, int cols,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// stacks of matrices, one box in one of them (segment_gemm.cuh)
-bool make_map_planes(CUtensorMap* m, const void* ptr, int type, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+// stacks of matrices, one box in one of them (segment_gemm.cuh): rows of `row_bytes` (128 or 64, swizzled over as many) x box_rows
+static bool make_map_boxes(CUtensorMap* m, const void* ptr, int type, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int row_bytes, int box_rows) {
     EncodeTiledFn enc = encoder();
     if (!enc) return false;
     const CUtensorMapDataType types[3] = {CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_DATA_TYPE_FLOAT32};
     const cuuint64_t size = type == 0 ? 2 : type == 1 ? 1 : 4;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * size, (cuuint64_t)rows * (cuuint64_t)ld * size};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)(row_bytes / size), (cuuint32_t)box_rows, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
-    return enc(m, types[type], 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return enc(m, types[type], 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool make_map_planes(CUtensorMap* m, const void* ptr, int type, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    return make_map_boxes(m, ptr, type, planes, rows, cols, ld, 128, box_rows);
+}
+bool make_map_rows_out(CUtensorMap* m, void* ptr, int type, int64_t rows, int64_t cols) { return make_map_boxes(m, ptr, type, 1, rows, cols, cols, 64, 32); }
 
 static int up16(int x) { return (x + 15) & ~15; }
 static int up32(int x) { return (x + 31) & ~31; }

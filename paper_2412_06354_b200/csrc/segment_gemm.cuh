@@ -75,6 +75,7 @@ struct SegGemmParams {
     int rows_out, cols_out;  // output rows that exist (SG_DW: features), output columns
     void* out;               // rows cols_out elements apart; SG_DW: [G, rows_out, cols_out]
     int vec;                 // rows of out start on 16 bytes
+    int bulk;                // whole boxes of 32 rows x 64 bytes leave by bulk stores through mapO (SG_DW: of the partials)
     float* part;             // SG_DW: partials [2 * parts][rows_out][cols_out]
     const float* bias;       // [G, cols_out] or nullptr
     const float* sx;         // SG_I8: scales of the rows, of the columns
@@ -296,6 +297,25 @@ __device__ __forceinline__ void sg_rows_out(uint32_t stg, T* out, int64_t ld, in
     }
 }
 
+// ... or, where all 32 rows exist, by one bulk tensor store (columns past the last are clipped; the places of the chunks are those of
+// the copy engine's 64-byte swizzle), which runs on while the warp does: sg_staging_free before the next use, sg_stores_done at the end.
+// (65,536 x 1024 -> 1024 over 64 segments 138 -> 133 us, 170k x 256 -> 256 in 8 bits 32 -> 29 us.)
+__device__ __forceinline__ void sg_box_out(uint32_t stg, const CUtensorMap* map, int x, int y, int lane) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(stg) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+__device__ __forceinline__ void sg_staging_free(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void sg_stores_done(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
 // rows of no segment: zeros, by the epilogue warps (threads from 64 on)
 template <int WARPS, typename T>
 __device__ __forceinline__ void sg_zero_outside(const SegGemmParams& P, T* out) {
@@ -322,7 +342,8 @@ __device__ __forceinline__ uint4 sg_pack(const float* f, const __nv_bfloat16*, u
 
 template <int MODE, typename T>
 __global__ void __launch_bounds__(SG_THREADS, 1)
-segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const SegGemmParams P) {
+segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
+                    const SegGemmParams P) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzle atoms lie on 1024 bytes
     __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 8];  // full[S], empty[S], acc_full[2], acc_empty[2], b_full[2], b_empty[2]
     __shared__ __align__(16) float s_cols[MODE == SG_I8 ? 2 : 1][256];                 // bias and column scales of the tile, zeros past the last
@@ -533,7 +554,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(r[q]);
                     }
                 };
-                auto send = [&](auto* out, int64_t ld, bool vec) {
+                auto send = [&](auto* out, int64_t ld, bool vec, bool bulk, int y) {
                     using O = typename std::remove_pointer<decltype(out)>::type;
                     constexpr int WIDE = 64 / sizeof(O), PER = Chunk<O>::N;  // columns of a staging row: 16 or 32; of a chunk
                     for (int cb = sub; cb * WIDE < bn; cb += SG_EPI_WARPS / 4) {
@@ -543,15 +564,19 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         for (int h = 0; h < WIDE / 16; ++h) tmem_ld16(taddr + (uint32_t)(cb * WIDE + h * 16), r + h * 16);
                         tmem_ld_wait();
                         float f[WIDE];
-                        __syncwarp();
+                        sg_staging_free(lane);
 #pragma unroll
                         for (int q = 0; q < WIDE / PER; ++q) {
 #pragma unroll
                             for (int k = 0; k < PER; k += 4) finish4(cb * WIDE + q * PER + k, r + q * PER + k, f + q * PER + k);
                             sg_stage(stg, lane, q, MODE == SG_DW || MODE == SG_DX ? Chunk<O>::pack(f + q * PER) : sg_pack(f + q * PER, (O*)nullptr, floor));
                         }
-                        __syncwarp();
-                        sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
+                        if (bulk && rows == 32) {
+                            sg_box_out(stg, &mapO, c_base + cb * WIDE, y, lane);
+                        } else {
+                            __syncwarp();
+                            sg_rows_out<O>(stg, out, ld, rows, c_base + cb * WIDE, c_end, vec, lane);
+                        }
                     }
                 };
                 if constexpr (MODE == SG_DW) {
@@ -560,12 +585,12 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     if (cut) {
                         // cut at the part's start: partial 2p, else (at its end) 2p + 1
                         const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
-                        send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0);
+                        send(P.part + which * size + off, P.cols_out, P.cols_out % 4 == 0, P.bulk != 0, (int)(which * P.rows_out) + mb * 128 + quarter * 32);
                     } else {
-                        send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0);
+                        send((T*)P.out + t.g * size + off, P.cols_out, P.vec != 0, false, 0);
                     }
                 } else {
-                    send((T*)P.out + row0 * P.cols_out, P.cols_out, P.vec != 0);
+                    send((T*)P.out + row0 * P.cols_out, P.cols_out, P.vec != 0, P.bulk != 0, (int)row0);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -575,6 +600,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
             ++lt;
             return true;
         });
+        sg_stores_done(lane);
         if (MODE == SG_Y || MODE == SG_DX) sg_zero_outside<SG_EPI_WARPS>(P, (T*)P.out);
     }
     if (failed) atomicExch(P.status, 7);  // GNN_ERR_TIMEOUT
@@ -587,9 +613,17 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 // rows of one plane, swizzled; out-of-range reads give zeros (linear_tma.cu)
 // type: 0 bf16, 1 bytes, 2 fp32
 bool make_map_planes(CUtensorMap* m, const void* ptr, int type, int64_t planes, int64_t rows, int64_t cols, int64_t ld, int box_rows);
+// what sg_box_out stores through: rows on 16 bytes
+bool make_map_rows_out(CUtensorMap* m, void* ptr, int type, int64_t rows, int64_t cols);
 bool tensor_map_encoder_available();
 // SG_Y, SG_DX or SG_DW of fp32 (segment_gemm_f32.cu); slot: of allow_big_smem
-gnn_status segment_gemm_f32(const char* who, int mode, int slot, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st);
+gnn_status segment_gemm_f32(const char* who, int mode, int slot, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, int64_t part_rows_all, cudaStream_t st);
+// the output's map, or that of the partials (SG_DW); other is passed in its place where rows do not start on 16 bytes
+inline bool sg_out_map(CUtensorMap* m, const CUtensorMap& other, SegGemmParams& P, void* ptr, int type, int64_t rows) {
+    P.bulk = (size_t)P.cols_out * (type == 0 ? 2 : 4) % 16 == 0;
+    *m = other;
+    return !P.bulk || make_map_rows_out(m, ptr, type, rows, P.cols_out);
+}
 
 // output columns of a tile: as few blocks of at most `most` as cover them, evened out, in steps of 64; halved while there are
 // fewer tiles than SMs (a tile's weights then arrive through more SMs)
@@ -601,7 +635,7 @@ inline int sg_block(int cols, int most, int64_t row_tiles) {
 }
 
 // How the tiles of SG_Y, SG_DX and SG_I8 are dealt out (see above).  Pairs: where the weights of a tile are too many to stay, contractions of
-// eight slices and a tile of 256 rows for every SM (65,536 x 1024 -> 1024 over 64 segments: XX us in ones, XX in pairs).
+// eight slices and a tile of 256 rows for every SM (65,536 x 1024 -> 1024 over 64 segments: 144 us in ones, 138 in pairs, both with stores by the warps).
 // Otherwise ranges where all weights together are a fraction of L2 and the rows give every SM a few tiles.
 inline bool sg_stays(const SegGemmParams& P) { return SG_EPI_WARPS * SG_STAGING + (size_t)P.bn * 128 * P.slices + 4 * SG_A_BYTES <= SG_SMEM_MAX; }
 inline void sg_deal(SegGemmParams& P, size_t weight_bytes, bool pairs = true) {
@@ -617,8 +651,11 @@ inline void sg_deal(SegGemmParams& P, size_t weight_bytes, bool pairs = true) {
 }
 
 template <int MODE, typename T>
-static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st) {
+static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, int64_t part_rows_all, cudaStream_t st) {
     const auto kernel = segment_gemm_kernel<MODE, T>;
+    CUtensorMap mapO;
+    if (MODE == SG_DW ? !sg_out_map(&mapO, mapA, P, P.part, 2, part_rows_all) : !sg_out_map(&mapO, mapA, P, P.out, sizeof(T) == 2 ? 0 : 2, P.N))
+        GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
     const gnn_status rc = allow_big_smem(who, (const void*)kernel, which, SG_SMEM_MAX);
     if (rc != GNN_OK) return rc;
     const size_t fixed = SG_EPI_WARPS * SG_STAGING, b_bytes = (size_t)P.bn * 128, tile = MODE == SG_DW ? 0 : b_bytes * P.slices;
@@ -630,7 +667,7 @@ static gnn_status sg_launch(const char* who, int which, const CUtensorMap& mapA,
     int cols = 32;
     while (cols < 2 * P.bn) cols <<= 1;
     P.tmem_cols = cols;
-    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SG_THREADS), fixed + held + (size_t)P.stages * slot, st, mapA, mapB, P);
+    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SG_THREADS), fixed + held + (size_t)P.stages * slot, st, mapA, mapB, mapO, P);
     GNN_CHECK_LAUNCH(who);
     return GNN_OK;
 }

@@ -80,7 +80,8 @@ __device__ __forceinline__ void sf_split32(float* x, uint32_t to) {
 
 template <int MODE>
 __global__ void __launch_bounds__(SF_THREADS, 1)
-segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const SegGemmParams P, const SegGemmF32Layout L) {
+segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
+                        const SegGemmParams P, const SegGemmF32Layout L) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     // r_full, r_empty [raw], b_full, b_empty [b], o_full, o_empty [groups], acc_full, acc_empty [2]
     __shared__ __align__(8) uint64_t bars[2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + 4];
@@ -313,15 +314,19 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             const int64_t left = MODE == SG_DW ? (int64_t)P.rows_out - mb * 128 - quarter * 32 : t.hi - t.lo - quarter * 32;
             const int rows = (int)(left < 32 ? left : 32), c_base = nb * bn;
             float* out = (float*)P.out;
-            bool vec = P.vec != 0;
+            bool vec = P.vec != 0, bulk = P.bulk != 0;
+            int y = (int)(t.lo + quarter * 32);
             if constexpr (MODE == SG_DW) {
                 const int64_t size = (int64_t)P.rows_out * P.cols_out;
                 if (t.a != t.lo || t.b != t.hi) {
                     // cut at the part's start: partial 2p, else (at its end) 2p + 1
-                    out = P.part + (2 * part + (t.a >= part * P.part_rows ? 1 : 0)) * size;
+                    const int64_t which = 2 * part + (t.a >= part * P.part_rows ? 1 : 0);
+                    out = P.part + which * size;
                     vec = P.cols_out % 4 == 0;
+                    y = (int)(which * P.rows_out) + mb * 128 + quarter * 32;
                 } else {
                     out += t.g * size;
+                    bulk = false;
                 }
                 out += (int64_t)(mb * 128 + quarter * 32) * P.cols_out;
             } else {
@@ -345,11 +350,15 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
 #pragma unroll
                     for (int q = 0; q < 16; ++q) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(f[q]));  // NaN stays
                 }
-                __syncwarp();
+                sg_staging_free(lane);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) sg_stage(stg, lane, q, Chunk<float>::pack(f + 4 * q));
-                __syncwarp();
-                sg_rows_out<float>(stg, out, P.cols_out, rows, c_base + cb * 16, P.cols_out, vec, lane);
+                if (bulk && rows == 32) {
+                    sg_box_out(stg, &mapO, c_base + cb * 16, y, lane);
+                } else {
+                    __syncwarp();
+                    sg_rows_out<float>(stg, out, P.cols_out, rows, c_base + cb * 16, P.cols_out, vec, lane);
+                }
             }
             tc_fence_before();
             __syncwarp();
@@ -357,6 +366,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
             ++lt;
             return true;
         });
+        sg_stores_done(lane);
         if (MODE != SG_DW) sg_zero_outside<SF_EPI_WARPS>(P, (float*)P.out);
     }
     if (failed) atomicExch(P.status, 7);  // GNN_ERR_TIMEOUT
@@ -366,8 +376,10 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
 }
 
 template <int MODE>
-static gnn_status sf_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st) {
+static gnn_status sf_launch(const char* who, int which, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, int64_t part_rows_all, cudaStream_t st) {
     const auto kernel = segment_gemm_f32_kernel<MODE>;
+    CUtensorMap mapO;
+    if (!sg_out_map(&mapO, mapA, P, MODE == SG_DW ? (void*)P.part : P.out, 2, MODE == SG_DW ? part_rows_all : P.N)) GNN_FAIL(GNN_ERR_CUDA, "%s: tensor map encoding failed", who);
     const gnn_status rc = allow_big_smem(who, (const void*)kernel, which, SG_SMEM_MAX);
     if (rc != GNN_OK) return rc;
     const size_t fixed = SF_EPI_WARPS * SG_STAGING;
@@ -388,13 +400,14 @@ static gnn_status sf_launch(const char* who, int which, const CUtensorMap& mapA,
         const size_t slots = (room - SF_RAW_SLOTS * (size_t)L.raw_bytes) / L.b_bytes;
         L.b_slots = slots < SF_B_SLOTS ? (int)slots : SF_B_SLOTS;
     }
-    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SF_THREADS), fixed + (size_t)L.raw_slots * L.raw_bytes + (size_t)L.b_slots * L.b_bytes, st, mapA, mapB, P, L);
+    launch_overlapped(kernel, dim3((unsigned)(P.units < 148 ? P.units : 148)), dim3(SF_THREADS), fixed + (size_t)L.raw_slots * L.raw_bytes + (size_t)L.b_slots * L.b_bytes, st, mapA, mapB, mapO, P, L);
     GNN_CHECK_LAUNCH(who);
     return GNN_OK;
 }
 
-gnn_status segment_gemm_f32(const char* who, int mode, int slot, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, cudaStream_t st) {
-    return mode == SG_Y ? sf_launch<SG_Y>(who, slot, mapA, mapB, P, st) : mode == SG_DX ? sf_launch<SG_DX>(who, slot, mapA, mapB, P, st) : sf_launch<SG_DW>(who, slot, mapA, mapB, P, st);
+gnn_status segment_gemm_f32(const char* who, int mode, int slot, const CUtensorMap& mapA, const CUtensorMap& mapB, SegGemmParams& P, int64_t part_rows_all, cudaStream_t st) {
+    return mode == SG_Y ? sf_launch<SG_Y>(who, slot, mapA, mapB, P, 0, st)
+         : mode == SG_DX ? sf_launch<SG_DX>(who, slot, mapA, mapB, P, 0, st) : sf_launch<SG_DW>(who, slot, mapA, mapB, P, part_rows_all, st);
 }
 
 }  // namespace gnn
