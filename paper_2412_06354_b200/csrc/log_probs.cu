@@ -185,7 +185,7 @@ struct LpParams {
 
 // what a row answers, from its statistics (all lanes) and its best (a lane each)
 template <typename T>
-__device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const LpStats& st, uint64_t best, int lane) {
+__device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const LpStats& st, float z_label, uint64_t best, int lane) {
     const float nan = __uint_as_float(0x7FC00000u);
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
     const float tail = log1pf(st.s);
@@ -197,7 +197,7 @@ __device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const 
         if (P.entropy) P.entropy[row] = bad ? nan : none ? 0.f : tail - st.t / (1.f + st.s);
         if (P.logp) {
             const int y = P.label[row];
-            P.logp[row] = y >= 0 && y < P.C ? logp((float)((const T*)P.z)[row * P.C + y]) : 0.f;
+            P.logp[row] = y >= 0 && y < P.C ? logp(z_label) : 0.f;
         }
     }
     if (lane < P.top) {
@@ -382,14 +382,16 @@ __device__ __forceinline__ float lp_chunk_max(uint4 v) {
 // threads' own largest scores is a floor of the k-th best class; only chunks that reach it are looked at again (in L1 or L2),
 // about k of thousands, and what reaches it in them is sorted.  Where that gives fewer than k classes or more than LP_CAND (many
 // equal scores, rows masked nearly throughout, scores that are not numbers) the classes are offered to a sorted list one by
-// one.  (Offered one by one always, 256 x 170,000 bf16, ten best: 175 us.)
+// one.  256 x 170,000 bf16, ten best: 31 us, 175 us with all offered one by one.  Chunks
+// fetched a step ahead, through shared memory or registers, other numbers of parts, or a maximum of which the sums follow only every
+// e^2: 33 to 44 us; a part's results pushed to the first block instead of fetched by it: 34 us.
 constexpr int LP_CAND = 256;
 constexpr int LP_CHUNKS = 48;  // chunks of a thread at most: shared memory
 
 template <typename T, int W, bool CLUSTER>
 __global__ void __launch_bounds__(256)
 log_probs_kernel(const LpParams P) {
-    pdl_wait();
+    if constexpr (W == 1) pdl_wait(); else pdl_wait_exclusive();  // (blocks of the next kernel that come up early lie unevenly)
     constexpr int PER = Chunk<T>::N;
     extern __shared__ float sh_max[];  // [chunks of a thread][256]
     __shared__ LpStats sh_stats[8];
@@ -423,6 +425,11 @@ log_probs_kernel(const LpParams P) {
         for (int k = 0; k < PER; ++k) x.e[k] = c0 * PER + (int64_t)i * PER + k < all ? zc[(int64_t)i * PER + k] : T(0.f);
         return x.q;
     };
+    float z_label = 0.f;  // (asked for here, not at the end, where it would be waited for)
+    if (part == 0 && me == 0 && P.logp) {
+        const int y = P.label[row];
+        if (y >= 0 && y < P.C) z_label = (float)z[e0 + y];
+    }
     auto inside = [&](int i, int k) { return (unsigned)(first_class + i * PER + k) < (unsigned)P.C; };
     auto scores = [&](int i, uint4 v, float* f) {  // those of other rows: -inf
         Chunk<T>::unpack(v, f);
@@ -544,13 +551,19 @@ log_probs_kernel(const LpParams P) {
     }
     uint64_t best = 0;
     if (list) {
-        float floor = lp_sort(mine, lane);
+        float floor = mine;
         const int g = W == 1 ? warp : 0;
         if (lane == 0) sh_count[warp] = 0;
         if constexpr (W == 1) {
-            floor = __shfl_sync(0xFFFFFFFFu, floor, P.top - 1);
+            floor = __shfl_sync(0xFFFFFFFFu, lp_sort(floor, lane), P.top - 1);
             __syncwarp();
+        } else if (P.top <= 16) {  // the k-th largest of 32 groups of eight threads will do: half as many groups more reach it, by chance, than classes are listed
+            sh_sorted[warp][lane] = mine;
+            __syncthreads();
+            for (int w = 0; w < W; ++w) floor = fmaxf(floor, sh_sorted[w][lane]);
+            floor = __shfl_sync(0xFFFFFFFFu, lp_sort(floor, lane), P.top - 1);
         } else {
+            floor = lp_sort(floor, lane);
             sh_sorted[warp][lane] = floor;
             __syncthreads();
             if (warp == 0) {
@@ -623,7 +636,7 @@ log_probs_kernel(const LpParams P) {
             return;
         }
     }
-    lp_finish<T>(P, row, st, best, lane);
+    lp_finish<T>(P, row, st, z_label, best, lane);
 }
 
 // The parts of a row joined: a block per row.  Only parts whose best class is among the k best such can hold one of the k best.
@@ -682,7 +695,7 @@ log_probs_join_kernel(const LpParams P) {
     }
     if (warp != 0) return;
     st = lp_join_warps(sh_stats, lane);
-    lp_finish<T>(P, row, st, P.top > 0 ? lp_best_of(sh_cand, sh_count, lane) : 0, lane);
+    lp_finish<T>(P, row, st, lane == 0 && P.logp && (unsigned)P.label[row] < (unsigned)P.C ? (float)((const T*)P.z)[row * P.C + P.label[row]] : 0.f, P.top > 0 ? lp_best_of(sh_cand, sh_count, lane) : 0, lane);
 }
 
 struct LpGradParams {
