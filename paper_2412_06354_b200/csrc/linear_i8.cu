@@ -39,7 +39,7 @@ struct RowScale {
         float q = fmaf(x, i, Q_MAGIC) - Q_MAGIC;
         const float r = 2.f * fmaf(-q, s, x), a = fabsf(r);
         if (a > s || (a == s && ((int)q & 1))) q += r > 0.f ? 1.f : -1.f;
-        return (int)q;
+        return (int)fminf(fmaxf(q, -127.f), 127.f);  // a subnormal scale may be rounded down so far that more steps fit
     }
 };
 

@@ -173,3 +173,17 @@ def test_replayed_graph_and_second_stream(gnn, n):
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(bits(out), bits(y))
+
+
+@pytest.mark.parametrize("K", [64, 61])
+def test_scales_with_few_digits(gnn, K):
+    """Rows of the smallest subnormals: the scale is a few units of 2^-149, rounded down by up to a third, and the quotient of the
+    largest value passes 127."""
+    import torch
+    unit = torch.arange(1, 401, dtype=torch.float64)[:, None] * (1 - 2 * (torch.arange(K, dtype=torch.float64) % 2)) * torch.linspace(0, 1, K, dtype=torch.float64).flip(0)
+    X = (unit.round() * 2.0 ** -149).float()
+    q, scale = gnn.quantize_rows(X.cuda())
+    rq, rs = rounded(X)
+    assert int(rq.abs().max()) > 127  # the oracle's quotients do pass it
+    assert torch.equal(q.long().cpu(), rq.clamp(-127, 127))
+    assert torch.equal(scale.double().cpu(), rs)
