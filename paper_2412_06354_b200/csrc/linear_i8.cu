@@ -198,7 +198,7 @@ static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scal
         return;
     }
     // four chunks per lane where the row has them: what a row costs once (the scale, the maximum over its lanes) is shared by 32 values
-    // (170,000 x 256 bf16, two chunks per lane: 33.7 us)
+    // (170,000 x 256 bf16: 23.7 us, 5.5 TB/s; two chunks per lane: 33.7 us)
     if (chunks <= 4) run(quantize_rows_kernel<T, 4, 1>, 4);
     else if (chunks <= 8) run(quantize_rows_kernel<T, 4, 2>, 4);
     else if (chunks <= 16) run(quantize_rows_kernel<T, 4, 4>, 4);
@@ -210,7 +210,8 @@ static void launch_quantize(const T* X, int64_t N, int K, int8_t* q, float* scal
 }
 
 // ------------------------------------------------------------------ the product
-// A few rows: a warp per output channel and four rows, four products to an instruction.  Bound by reading the weights once.
+// A few rows: a warp per output channel and four rows, four products to an instruction.  Bound by reading the weights once: one row,
+// 1024 x 1024, 4.3 us, of which about 2.5 are the launch.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 linear_i8_rows_kernel(const int8_t* xq, const float* sx, const int8_t* wq, const float* sw, int N, int K, int M, const float* bias, int relu, T* __restrict__ Y, int* status) {
