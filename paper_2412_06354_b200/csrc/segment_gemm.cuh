@@ -140,6 +140,12 @@ struct SegCursor {
 
 // a bounded wait of a whole warp, with one answer
 __device__ __forceinline__ bool sg_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity)); }
+// a meeting of as many warps as bar counts, the met-th at this barrier: as bar.sync, but with a limit (a warp that gave up does not come)
+__device__ __forceinline__ bool sg_meet(uint32_t bar, uint32_t met) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+    return sg_wait(bar, met & 1u);
+}
 // a place in a ring of n slots and the parity of its round (counted, not divided: n is known at run time only)
 struct SgRing {
     uint32_t n, s, parity, uses;
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(SG_THREADS, 1)
 segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
                     const SegGemmParams P) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzle atoms lie on 1024 bytes
-    __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 8];  // full[S], empty[S], acc_full[2], acc_empty[2], b_full[2], b_empty[2]
+    __shared__ __align__(8) uint64_t bars[2 * SG_MAX_STAGES + 9];  // full[S], empty[S], acc_full[2], acc_empty[2], b_full[2], b_empty[2], meet
     __shared__ __align__(16) float s_cols[MODE == SG_I8 ? 2 : 1][256];                 // bias and column scales of the tile, zeros past the last
     __shared__ uint32_t tmem_base_slot;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -370,10 +376,12 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     auto acc_empty = [&](uint32_t a) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 2 + a); };
     auto b_full = [&](uint32_t b) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 4 + b); };
     auto b_empty = [&](uint32_t b) { return bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 6 + b); };
+    const uint32_t meet = bar0 + 8u * (uint32_t)(2 * SG_MAX_STAGES + 8);
 
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SG_EPI_WARPS); mbar_init(b_full(a), 1); mbar_init(b_empty(a), 1); }
+        mbar_init(meet, SG_EPI_WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
@@ -515,17 +523,17 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;  // tensor-memory lanes 32 * (warp % 4)..: hardware rule
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
         const uint32_t floor = P.relu ? 0u : 0xFF80FF80u;
-        uint32_t lt = 0, second = 0;
+        uint32_t lt = 0, second = 0, met = 0;
         int staged_g = -1, staged_n = -1;
         walk([&](const SegRows& t, int mb, int nb, int64_t part) {
             if ((MODE == SG_Y || MODE == SG_I8) && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
-                asm volatile("bar.sync 1, 512;" ::: "memory");
+                if (!sg_meet(meet, met++)) { failed = true; return false; }
                 if (c < 256) {
                     s_cols[0][c] = P.bias && c < bn && col < P.cols_out ? P.bias[(int64_t)t.g * P.cols_out + col] : 0.f;
                     if constexpr (MODE == SG_I8) s_cols[1][c] = c < bn && col < P.cols_out ? P.sw[col] : 0.f;
                 }
-                asm volatile("bar.sync 1, 512;" ::: "memory");
+                if (!sg_meet(meet, met++)) { failed = true; return false; }
                 staged_g = t.g;
                 staged_n = nb;
             }

@@ -85,8 +85,8 @@ __global__ void __launch_bounds__(SF_THREADS, 1)
 segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
                         const SegGemmParams P, const SegGemmF32Layout L) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    // r_full, r_empty [raw], b_full, b_empty [b], o_full, o_empty [groups], acc_full, acc_empty [2]
-    __shared__ __align__(8) uint64_t bars[2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + 4];
+    // r_full, r_empty [raw], b_full, b_empty [b], o_full, o_empty [groups], acc_full, acc_empty [2], meet
+    __shared__ __align__(8) uint64_t bars[2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + 5];
     __shared__ __align__(16) float s_bias[128];
     __shared__ uint32_t tmem_base_slot, s_raw[SF_RAW_SLOTS], s_op[SF_GROUPS];  // what the slice of a slot, of an operand buffer is
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -107,6 +107,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
     auto o_empty = [&](uint32_t o) { return bar0 + 8u * (2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + SF_GROUPS + o); };
     auto acc_full = [&](uint32_t a) { return bar0 + 8u * (2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + a); };
     auto acc_empty = [&](uint32_t a) { return bar0 + 8u * (2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + 2 + a); };
+    const uint32_t meet = bar0 + 8u * (2 * SF_RAW_SLOTS + 2 * SF_B_SLOTS + 2 * SF_GROUPS + 4);
     const uint32_t nraw = (uint32_t)L.raw_slots, nb_slots = (uint32_t)L.b_slots, nacc = (uint32_t)L.acc_bufs;
 
     if (tid == 0) {
@@ -114,6 +115,7 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
         for (uint32_t s = 0; s < nb_slots; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), 1); }
         for (uint32_t o = 0; o < SF_GROUPS; ++o) { mbar_init(o_full(o), SF_GROUP_WARPS); mbar_init(o_empty(o), 1); }
         for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), SF_EPI_WARPS); }
+        mbar_init(meet, SF_EPI_WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mapB)) : "memory");
@@ -298,15 +300,15 @@ segment_gemm_f32_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_c
     } else {
         const int ew = warp - 2, quarter = warp & 3, sub = ew >> 2;
         const uint32_t stg = stage0 + (uint32_t)ew * SG_STAGING;
-        uint32_t lt = 0;
+        uint32_t lt = 0, met = 0;
         int staged_g = -1, staged_n = -1;
         sg_walk<MODE>(P, [&](const SegRows& t, int mb, int nb, int64_t part) {
             const uint32_t a = two_acc ? lt & 1u : 0u;
             if (MODE == SG_Y && P.bias && (t.g != staged_g || nb != staged_n)) {  // the same in all epilogue warps
                 const int c = tid - 64, col = nb * bn + c;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (!sg_meet(meet, met++)) { failed = true; return false; }
                 if (c < 128) s_bias[c] = c < bn && col < P.cols_out ? P.bias[(int64_t)t.g * P.cols_out + col] : 0.f;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (!sg_meet(meet, met++)) { failed = true; return false; }
                 staged_g = t.g;
                 staged_n = nb;
             }

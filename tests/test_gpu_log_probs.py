@@ -250,7 +250,7 @@ def test_gradient_against_differences(gnn):
     assert abs(slope - want) <= room
 
 
-@pytest.mark.parametrize("n,C", [(300, 47), (5, 60000)])
+@pytest.mark.parametrize("n,C", [(300, 47), (5, 60000), (200, 20000), (5000, 47)])
 def test_replayed_graph_and_second_stream(gnn, n, C):
     import torch
     zs = [scores(n, C, "bf16", q)[0].cuda() for q in range(3)]
