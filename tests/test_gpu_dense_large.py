@@ -102,3 +102,35 @@ def test_log_probs(gnn, C):
     ref[torch.arange(len(rows)), y.long()] += 1.0
     room = 2.0 * (4e-6 + 2.0 ** -22 * rl.abs()[:, None] + 2.0 ** -22 * lp.abs()) * p + 2.0 ** -23 * ref.abs() + 1e-38
     near(dZ[rows], ref, room + 2.0 ** -8 * (ref.abs() + room), "dZ")
+
+
+@pytest.mark.parametrize("dtype,K,M", [("bf16", 8192, 8192), ("bf16", 8191, 24), ("bf16", 40, 8190), ("f32", 2048, 2048), ("f32", 2047, 20), ("f32", 33, 2046)])
+def test_widest_matrices(gnn, dtype, K, M):
+    """The largest K and M that are taken, and their neighbours: whole numbers again, sums under 2^15, one rounding to bf16."""
+    import torch
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    sizes = [3, 0, 150, 140]
+    ptr = torch.tensor([0, 3, 3, 153, 293], device="cuda")
+    X, W, dY = whole(293, K, 5, t), whole(4 * K, M, 6, t).view(4, K, M), whole(293, M, 7, t)
+    Y = gnn.linear_segments(X, ptr, W)
+    dX, dW = gnn.linear_segments_backward(X, ptr, W, dY)
+    a = 0
+    for g, n in enumerate(sizes):
+        x, w, dy = (v.double() for v in (X[a:a + n], W[g], dY[a:a + n]))
+        assert torch.equal(Y[a:a + n], (x @ w).to(t)), g
+        assert torch.equal(dX[a:a + n], (dy @ w.t()).to(t)), g
+        assert torch.equal(dW[g], (x.t() @ dy).to(t)), g
+        a += n
+
+
+@pytest.mark.parametrize("n", [5, 200])
+def test_longest_8_bit_sums(gnn, n):
+    """K = 131071: random values (sums far under 2^24, one rounding) and one row of the extremes (a sum of nearly 2^31, rounded to 24 bits)."""
+    import torch
+    K, M = 131071, 70
+    g = torch.Generator("cuda").manual_seed(n)
+    x = torch.randint(-3, 4, (n, K), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-3, 4, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    x[0], w[0] = -128, -128
+    Y = gnn.linear_i8(x, torch.ones(n, device="cuda"), w, torch.ones(M, device="cuda"), dtype=torch.float32)
+    assert torch.equal(Y, (x.double() @ w.double().t()).float())
