@@ -144,7 +144,8 @@ struct LpRun {
     __device__ __forceinline__ void raise(float v) {
         const bool first = m == -INFINITY;
         k.x = k.y = fabsf(v) > 1e37f ? 0.25f : LOG2E;
-        const float q = v * k.x, d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
+        // (rounded as r is before it is taken from r: in one instruction with that the sums would stand for another r than the next ones')
+        const float q = __fmul_rn(v, k.x), d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
         t = first ? make_float2(0.f, 0.f) : make_float2(f * fmaf(d, s.x, t.x), f * fmaf(d, s.y, t.y));
         s = make_float2(f * s.x, f * s.y);  // (not a number stays one)
         m = v;
