@@ -123,15 +123,19 @@ __device__ __forceinline__ uint64_t lp_best_of(const uint64_t* keys, int n, int 
 
 // Running sums of one thread: r = m log2(e) rounded, s = sum of 2^(z log2(e) - r) over all of its classes, t the same weighted by the
 // exponent.  Two classes at a time (packed fp32 instructions).  z log2(e) - r is one rounding off whatever m is; what r itself is off
-// by is taken out at the end.  Beyond |m| = 1e37, where m log2(e) could overflow, neighbouring numbers are 1e30 apart: 2^(z / 4 - m / 4)
-// tells as well who is at m, and all others are 0.
+// by (1 at most up to |m| = 2^24) is taken out at the end.  A row whose largest score is beyond FAR is summed again from its threads'
+// maxima, the exponent as (z - m) log2(e): exact there, an instruction more per pair.  What the threads' first sums have to be
+// until then is finite, since masks (-1e9 or -1e30, say) may come before the scores of a nearer row: up to 2^30 r is off by 64 at most;
+// beyond, where m log2(e) could be off by more than an exponent holds, neighbouring numbers are 128 apart: 2^(z - m) tells as well who is at
+// m, and all others are 0.
 struct LpRun {
     float m, r;
-    float2 k, minus;  // the factor, and -r, twice each
+    float2 k, minus;  // the factor, and -r (from_maximum: -m), twice each
     float2 s, t;
-    static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+    bool exact;       // from_maximum
+    static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, FAR = 16777216.f, LIMIT = 1073741824.f;
     __device__ __forceinline__ void clear() {
-        m = -INFINITY; r = 0.f;
+        m = -INFINITY; r = 0.f; exact = false;
         k = make_float2(LOG2E, LOG2E);
         minus = s = t = make_float2(0.f, 0.f);
     }
@@ -142,19 +146,28 @@ struct LpRun {
     }
     // the maximum becomes v > m
     __device__ __forceinline__ void raise(float v) {
-        const bool first = m == -INFINITY;
-        k.x = k.y = fabsf(v) > 1e37f ? 0.25f : LOG2E;
+        const float factor = fabsf(v) > LIMIT ? 1.f : LOG2E;
+        const bool none = m == -INFINITY || factor != k.x;  // of the sums so far (another factor: v is 128 above m at least)
+        k.x = k.y = factor;
         // (rounded as r is before it is taken from r: in one instruction with that the sums would stand for another r than the next ones')
-        const float q = __fmul_rn(v, k.x), d = fmaxf(r - q, -2000.f), f = first ? 0.f : exp2_(d);
-        t = first ? make_float2(0.f, 0.f) : make_float2(f * fmaf(d, s.x, t.x), f * fmaf(d, s.y, t.y));
+        const float q = __fmul_rn(v, k.x), d = fmaxf(r - q, -2000.f), f = none ? 0.f : exp2_(d);
+        t = none ? make_float2(0.f, 0.f) : make_float2(f * fmaf(d, s.x, t.x), f * fmaf(d, s.y, t.y));
         s = make_float2(f * s.x, f * s.y);  // (not a number stays one)
         m = v;
         r = q;
         minus = make_float2(-q, -q);
     }
+    // the sums anew, by add<true>, for the largest score (or -inf: there is none)
+    __device__ __forceinline__ void from_maximum(float v) {
+        clear();
+        m = v;
+        exact = true;
+        if (v > -INFINITY) minus = make_float2(-v, -v);
+    }
     // two scores, neither above m; -inf: 2^-inf = 0 times a finite exponent
+    template <bool EXACT>
     __device__ __forceinline__ void add(float a, float b) {
-        const float2 u = fma2(make_float2(a, b), k, minus);
+        const float2 z = make_float2(a, b), u = EXACT ? fma2(add2(z, minus), make_float2(LOG2E, LOG2E), make_float2(0.f, 0.f)) : fma2(z, k, minus);
         const float2 e = make_float2(exp2_(u.x), exp2_(u.y));
         s = add2(s, e);
         t = fma2(e, make_float2(fmaxf(u.x, -2000.f), fmaxf(u.y, -2000.f)), t);
@@ -165,7 +178,7 @@ struct LpRun {
         const float S = s.x + s.y;
         o.m = m;
         if (!(m > -INFINITY) || m == INFINITY) { o.s = S == S && m < INFINITY ? 0.f : __uint_as_float(0x7FC00000u); o.t = 0.f; return o; }
-        const float off = fmaf(m, k.x, -r), f = exp2_(-off);
+        const float off = exact ? 0.f : fmaf(m, k.x, -r), f = exp2_(-off);
         o.s = taken_out ? f * S : fmaf(f, S, -1.f);
         o.t = LN2 * f * fmaf(-off, S, t.x + t.y);
         return o;
@@ -293,14 +306,17 @@ log_probs_few_kernel(const LpParams P) {
     // the sums without the leading class: at -inf meanwhile
     LpRun run;
     run.clear();
-    if (m > -INFINITY) {
-        run.raise(m);
-        mine[lead] = -INFINITY;
-    }
-    for (int g = 0; g < full; ++g)
+    if (m > -INFINITY) mine[lead] = -INFINITY;
+    if (fabsf(m) > LpRun::FAR && fabsf(m) < INFINITY) {
+        run.from_maximum(m);
+        for (int c = 0; c < C; ++c) run.add<true>(mine[c], -INFINITY);
+    } else {
+        if (m > -INFINITY) run.raise(m);
+        for (int g = 0; g < full; ++g)
 #pragma unroll
-        for (int c = 0; c < 8; c += 2) run.add(mine[8 * g + c], mine[8 * g + c + 1]);
-    for (int c = 8 * full; c < C; ++c) run.add(mine[c], -INFINITY);
+            for (int c = 0; c < 8; c += 2) run.add<false>(mine[8 * g + c], mine[8 * g + c + 1]);
+        for (int c = 8 * full; c < C; ++c) run.add<false>(mine[c], -INFINITY);
+    }
     if (lead < C) mine[lead] = nan;  // taken
     const LpStats st = run.stats(true);
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
@@ -466,7 +482,7 @@ log_probs_kernel(const LpParams P) {
                 float f[PER];
                 Chunk<T>::unpack(v[u], f);
 #pragma unroll
-                for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+                for (int k = 0; k < PER; k += 2) run.add<false>(f[k], f[k + 1]);
             }
             continue;
         }
@@ -485,7 +501,7 @@ log_probs_kernel(const LpParams P) {
             ++n;
             if (cm > run.m) run.raise(cm);
 #pragma unroll
-            for (int k = 0; k < PER; k += 2) run.add(f[k], f[k + 1]);
+            for (int k = 0; k < PER; k += 2) run.add<false>(f[k], f[k + 1]);
         }
     }
     const float mine = run.m;  // its own largest score
@@ -495,6 +511,23 @@ log_probs_kernel(const LpParams P) {
         if (lane == 0) sh_stats[warp] = st;
         __syncthreads();
         st = lp_join_warps(sh_stats, lane);
+    }
+    if (fabsf(st.m) > LpRun::FAR && fabsf(st.m) < INFINITY) {  // far from zero: once more, by exact differences
+        run.from_maximum(mine);
+        for (int c = me; c < count; c += STEP) {
+            float f[PER];
+            scores(c, load(c), f);
+#pragma unroll
+            for (int k = 0; k < PER; k += 2) run.add<true>(f[k], f[k + 1]);
+        }
+        st = run.stats();
+        lp_join_lanes(st, lane);
+        if constexpr (W > 1) {
+            __syncthreads();  // the first sums have been read
+            if (lane == 0) sh_stats[warp] = st;
+            __syncthreads();
+            st = lp_join_warps(sh_stats, lane);
+        }
     }
     // One class takes most of it: the sum beside its own 1 has lost digits in the thread that holds it.  That thread's chunks again,
     // without the 1, by its warp; the other threads' sums stand.
