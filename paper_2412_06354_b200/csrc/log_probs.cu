@@ -55,7 +55,7 @@ struct LpStats {
         if (o.m == -INFINITY) { s += o.s; return; }  // nothing in it, or not numbers only
         const float d = o.m - m, f = lp_exp(d), c = f * (o.s + 1.f);
         s += c;
-        t += fmaf(d, c, f * o.t);
+        t += fmaf(fmaxf(d, -1000.f), c, f * o.t);  // d = -inf: times 0
     }
 };
 

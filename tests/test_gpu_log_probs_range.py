@@ -103,3 +103,17 @@ def test_a_far_row_leaves_the_others_alone(gnn):
         keep = torch.cat([torch.arange(0, 1), torch.arange(2, n)]).cuda()
         for x, y in zip(a[1:], b[1:]):
             assert np.array_equal(bits(x[keep]), bits(y[keep]))
+
+
+@pytest.mark.parametrize("C", [60000, 1200000, 3000001])
+def test_parts_whose_maxima_lie_farther_apart_than_a_number_holds(gnn, C):
+    """The lowest value throughout and one score from which it is farther away than the largest fp32 number, so that the difference of
+    two parts' maxima is -inf (the longest rows have more parts than the joining block has lanes per warp and turn)."""
+    import torch
+    for big in (1e32, 3e38):
+        for at in (0, C // 2, C - 1):
+            Z = torch.full((1, C), torch.finfo(torch.float32).min)
+            Z[0, at] = big
+            logp, H, lse, tl, ti = gnn.log_probs(Z.cuda(), torch.tensor([at], dtype=torch.int32, device="cuda"), top=2)
+            assert float(logp) == 0.0 and float(H) == 0.0 and float(lse) == float(torch.tensor(big)) and ti[0].tolist() == [at, 1 if at == 0 else 0]
+            assert float(tl[0, 0]) == 0.0 and float(tl[0, 1]) == float("-inf")  # -6.4e38 and less: no fp32 number
