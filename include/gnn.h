@@ -565,7 +565,7 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
 
 /* dZ[i,c] = dlogp[i] ([c = label[i]] - p_c) - dentropy[i] p_c (log p_c + entropy[i]) with p_c = exp(Z[i,c] - lse[i]), of dtype.
  * lse and entropy are gnn_log_probs' outputs.  dlogp (float [N], needs label) and dentropy (float [N], needs entropy) may be
- * NULL; dlogp of a row without a label is not used.  A class at -inf gets 0 (its label's share excepted); a row whose
+ * NULL; dlogp of a row without a label is not used.  A class at -inf gets 0 (its label's share excepted; |dentropy| up to 1e36); a row whose
  * lse is under -1e30 (all classes at -inf, or at the type's lowest value) zeros.  dZ may be Z.
  * The listed best classes are not differentiated. */
 gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const float* lse, const float* entropy,

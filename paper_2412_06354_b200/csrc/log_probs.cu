@@ -754,10 +754,11 @@ struct LpRow {
         h = P.dentropy ? P.dentropy[row] : 0.f;
         H = P.dentropy ? P.entropy[row] : 0.f;
     }
-    // without the label's own share.  A class at -inf: p = 0 times a finite value
+    // without the label's own share.  A class at -inf: p = 0 times what is finite for all h up to 1e36 (p is 0 from log p = -88 on, so
+    // that the bound changes no other; a comparison of p instead: 2048 x 50,000 bf16 67 -> 71 us)
     __device__ __forceinline__ float operator()(float z) const {
         const float lp = z - lse;
-        return none ? 0.f : -lp_exp(lp) * fmaf(h, fmaxf(lp, -1e30f) + H, g);
+        return none ? 0.f : -lp_exp(lp) * fmaf(h, fmaxf(lp, -128.f) + H, g);
     }
 };
 
