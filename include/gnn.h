@@ -567,10 +567,23 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
  * lse and entropy are gnn_log_probs' outputs.  dlogp (float [N], needs label) and dentropy (float [N], needs entropy) may be
  * NULL; dlogp of a row without a label is not used.  A class at -inf gets 0 (its label's share excepted; |dentropy| up to 1e36); a row whose
  * lse is under -1e30 (all classes at -inf, or at the type's lowest value) zeros.  dZ may be Z.
- * The listed best classes are not differentiated. */
+ * The listed best classes are not differentiated.
+ * lse is rounded to fp32, so that every p of a row is off by up to half a unit of its last bit: 4e-6 of itself at |lse| = 100, 5e-4 at 1e4, all
+ * of it from about 1e7 on (a row masked throughout by -1e9, say), and 1 - p of a nearly sure label is lost.  The calls
+ * below do without that loss. */
 gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const float* lse, const float* entropy,
                                   const float* dlogp, const float* dentropy, int32_t N, int C, gnn_dtype dtype, void* dZ,
                                   gnn_stream stream);
+
+/* The same two calls with lse in two numbers: lse_rest (float [N], or NULL: as above) is what the rounding of lse leaves out, lse + lse_rest
+ * as exact as logp is (0 where lse is not finite).  Given it, the gradient uses log p_c = (Z[i,c] - lse[i]) - lse_rest[i], with
+ * -expm1(log p) for the label's 1 - p: right to fp32 wherever the scores lie. */
+gnn_status gnn_log_probs_rest(const void* Z, const int32_t* label, int32_t N, int C, gnn_dtype dtype, int top, float* logp,
+                              float* entropy, float* lse, float* lse_rest, float* top_logp, int32_t* top_idx, void* ws,
+                              size_t ws_bytes, gnn_stream stream);
+gnn_status gnn_log_probs_rest_backward(const void* Z, const int32_t* label, const float* lse, const float* lse_rest,
+                                       const float* entropy, const float* dlogp, const float* dentropy, int32_t N, int C,
+                                       gnn_dtype dtype, void* dZ, gnn_stream stream);
 
 /* ------------------------------------------------------------------ aggregate -> transform fusion */
 

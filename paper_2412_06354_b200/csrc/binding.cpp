@@ -1008,7 +1008,7 @@ FN(linear_i8) {
     return wanted ? wrap_all(Y, wt) : wrap(Y);
 }
 
-// (Z, label, top, want_entropy, ws) -> (logp, entropy, lse, top_logp, top_idx)
+// (Z, label, top, want_entropy, ws, return_rest) -> (logp, entropy, lse, top_logp, top_idx), with return_rest lse_rest too
 FN(log_probs) {
     const at::Tensor &Z = A.dev(0), &label = A.t(1);
     const OnDevice on(Z);
@@ -1021,24 +1021,26 @@ FN(log_probs) {
     const int c = size32(C);
     if (top < 0 || top > C) raise(PyExc_ValueError, "top must lie between 0 and the number of classes");
     const int32_t* y = i32(label, "label");
-    at::Tensor logp, entropy, lse = empty({N}, at::kFloat, Z.device());
+    const bool wanted = A.flag(5);
+    at::Tensor logp, entropy, rest, lse = empty({N}, at::kFloat, Z.device());
+    if (wanted) rest = empty({N}, at::kFloat, Z.device());
     if (label.defined()) logp = empty({N}, at::kFloat, Z.device());
     if (A.flag(3)) entropy = empty({N}, at::kFloat, Z.device());
     at::Tensor tl = empty({N, top}, at::kFloat, Z.device()), ti = empty({N, top}, at::kInt, Z.device());
     const size_t need = gnn_log_probs_workspace(n, c, (int)top, dt);
     Scratch ws(A.t(4), need, Z.device());
     const gnn_stream st = stream();
-    CALL(gnn_log_probs(ptr(Z), y, n, c, dt, (int)top, (float*)ptr(logp), (float*)ptr(entropy), (float*)ptr(lse), (float*)ptr(tl), (int32_t*)ptr(ti), ws.p, ws.n, st));
-    return wrap_all(logp, entropy, lse, tl, ti);
+    CALL(gnn_log_probs_rest(ptr(Z), y, n, c, dt, (int)top, (float*)ptr(logp), (float*)ptr(entropy), (float*)ptr(lse), (float*)ptr(rest), (float*)ptr(tl), (int32_t*)ptr(ti), ws.p, ws.n, st));
+    return wanted ? wrap_all(logp, entropy, lse, tl, ti, rest) : wrap_all(logp, entropy, lse, tl, ti);
 }
 
-// (Z, label, lse, dlogp, entropy, dentropy) -> dZ
+// (Z, label, lse, dlogp, entropy, dentropy, lse_rest) -> dZ
 FN(log_probs_backward) {
-    const at::Tensor &Z = A.dev(0), &label = A.t(1), &lse = A.dev(2), &dlogp = A.t(3), &entropy = A.t(4), &dentropy = A.t(5);
+    const at::Tensor &Z = A.dev(0), &label = A.t(1), &lse = A.dev(2), &dlogp = A.t(3), &entropy = A.t(4), &dentropy = A.t(5), &rest = A.t(6);
     const OnDevice on(Z);
     dims(Z, 2, "Z");
     const int64_t N = Z.size(0), C = Z.size(1);
-    for (const auto& [t, name] : {std::pair<const at::Tensor*, const char*>{&label, "label"}, {&lse, "lse"}, {&dlogp, "dlogp"}, {&entropy, "entropy"}, {&dentropy, "dentropy"}}) {
+    for (const auto& [t, name] : {std::pair<const at::Tensor*, const char*>{&label, "label"}, {&lse, "lse"}, {&dlogp, "dlogp"}, {&entropy, "entropy"}, {&dentropy, "dentropy"}, {&rest, "lse_rest"}}) {
         shaped(*t, {N}, name);
         on.same(*t, name);
     }
@@ -1046,10 +1048,10 @@ FN(log_probs_backward) {
     const int32_t n = rows32(N);
     const int c = size32(C);
     const int32_t* y = i32(label, "label");
-    const float *l = f32(lse, "lse"), *g = f32(dlogp, "dlogp"), *H = f32(entropy, "entropy"), *h = f32(dentropy, "dentropy");
+    const float *l = f32(lse, "lse"), *g = f32(dlogp, "dlogp"), *H = f32(entropy, "entropy"), *h = f32(dentropy, "dentropy"), *r = f32(rest, "lse_rest");
     at::Tensor dZ = empty_like(Z);
     const gnn_stream st = stream();
-    CALL(gnn_log_probs_backward(ptr(Z), y, l, H, g, h, n, c, dt, ptr(dZ), st));
+    CALL(gnn_log_probs_rest_backward(ptr(Z), y, l, r, H, g, h, n, c, dt, ptr(dZ), st));
     return wrap(dZ);
 }
 

@@ -11,6 +11,8 @@
 // score does not pass the worst of them is left alone.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "tc_common.cuh"
 
 namespace gnn {
@@ -190,12 +192,22 @@ struct LpParams {
     const int32_t* label;  // or nullptr
     int64_t N;
     int C, top;
-    float *logp, *entropy, *lse, *top_logp;  // each may be nullptr
+    float *logp, *entropy, *lse, *lse_rest, *top_logp;  // each may be nullptr
     int32_t* top_idx;
     int parts;          // blocks per row (whole-block rows)
     float* stats;       // [N][parts][4] where parts > 1
     uint64_t* keys;     // [N][parts][top]
 };
+
+// lse = m + log1p(s), and what its rounding leaves out (exactly: the sum of two numbers in two)
+__device__ __forceinline__ void lp_lse_out(const LpParams& P, int64_t row, float m, float tail, bool bad, bool none) {
+    const float lse = bad ? __uint_as_float(0x7FC00000u) : none ? -INFINITY : m + tail;
+    if (P.lse) P.lse[row] = lse;
+    if (P.lse_rest) {
+        const float b = lse - m;
+        P.lse_rest[row] = bad || none ? 0.f : (m - (lse - b)) + (tail - b);
+    }
+}
 
 // what a row answers, from its statistics (all lanes) and its best (a lane each)
 template <typename T>
@@ -203,11 +215,10 @@ __device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const 
     const float nan = __uint_as_float(0x7FC00000u);
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
     const float tail = log1pf(st.s);
-    const float lse = bad ? nan : none ? -INFINITY : st.m + tail;
     // z - lse as (z - m) - log1p(s): exact where z is the largest
     auto logp = [&](float z) { return bad ? nan : none || z == -INFINITY ? -INFINITY : (z - st.m) - tail; };
     if (lane == 0) {
-        if (P.lse) P.lse[row] = lse;
+        lp_lse_out(P, row, st.m, tail, bad, none);
         if (P.entropy) P.entropy[row] = bad ? nan : none ? 0.f : tail - st.t / (1.f + st.s);
         if (P.logp) {
             const int y = P.label[row];
@@ -322,7 +333,7 @@ log_probs_few_kernel(const LpParams P) {
     const bool bad = st.s != st.s || st.m == INFINITY, none = st.m == -INFINITY;
     const float tail = log1pf(st.s);
     auto logp = [&](float x) { return bad ? nan : none || x == -INFINITY ? -INFINITY : (x - st.m) - tail; };
-    if (P.lse) P.lse[row] = bad ? nan : none ? -INFINITY : st.m + tail;
+    lp_lse_out(P, row, st.m, tail, bad, none);
     if (P.entropy) P.entropy[row] = bad ? nan : none ? 0.f : tail - st.t / (1.f + st.s);
     if (P.logp) {
         const int y = P.label[row];
@@ -737,13 +748,18 @@ struct LpGradParams {
     const int32_t* label;
     int64_t N;
     int C;
-    const float *lse, *entropy, *dlogp, *dentropy;  // entropy and dentropy together, or neither; dlogp may be nullptr
+    const float *lse, *lse_rest, *entropy, *dlogp, *dentropy;  // entropy and dentropy together, or neither; dlogp may be nullptr
     void* dz;
 };
 
-// what a row's gradient needs; none: nothing to choose from, so that nothing depends on the scores
+// What a row's gradient needs; none: nothing to choose from, so that nothing depends on the scores.
+// REST: with what the rounding of lse left out.  z - lse is then off by its own rounding alone, not by half a unit of lse's last bit (of the row's
+// every p: 5e-4 at lse = 1e4, all of it from about 1e7 on), and a nearly sure label's 1 - p keeps its digits.
+// 2048 x 50,000 bf16 74 us, 170,000 x 47 fp32 27 us (without: 67 and 21); 20,000 x 2000 fp32 76 us (85).
+template <bool REST>
 struct LpRow {
-    float lse, H, g, h;
+    float lse, H, g, h;  // (REST: H less the rest, so that z - lse serves in both places, and the rest's share of the exponent)
+    float rest, shift;
     int y;
     bool none;
     __device__ __forceinline__ void read(const LpGradParams& P, int64_t row) {
@@ -753,20 +769,41 @@ struct LpRow {
         g = P.dlogp && y >= 0 && y < P.C && !none ? P.dlogp[row] : 0.f;
         h = P.dentropy ? P.dentropy[row] : 0.f;
         H = P.dentropy ? P.entropy[row] : 0.f;
+        if constexpr (REST) {
+            rest = P.lse_rest[row];
+            shift = rest * -1.4426950408889634f;
+            H -= rest;
+        }
     }
     // without the label's own share.  A class at -inf: p = 0 times what is finite for all h up to 1e36 (p is 0 from log p = -88 on, so
     // that the bound changes no other; a comparison of p instead: 2048 x 50,000 bf16 67 -> 71 us)
     __device__ __forceinline__ float operator()(float z) const {
         const float lp = z - lse;
-        return none ? 0.f : -lp_exp(lp) * fmaf(h, fmaxf(lp, -128.f) + H, g);
+        return none ? 0.f : -p(lp) * fmaf(h, fmaxf(lp, -128.f) + H, g);
     }
+    // (REST) the label, its share g (1 - p) included
+    __device__ __forceinline__ float at_label(float z) const {
+        const float lp = z - lse;
+        return none ? 0.f : -p(lp) * h * (fmaxf(lp, -128.f) + H) - expm1f(lp - rest) * g;
+    }
+    __device__ __forceinline__ float p(float lp) const { return REST ? LpRun::exp2_(fmaf(lp, 1.4426950408889634f, shift)) : lp_exp(lp); }
 };
+
+// element k of a chunk
+template <typename T>
+__device__ __forceinline__ float lp_pick(uint4 v, int k) {
+    float f[Chunk<T>::N], x = 0.f;
+    Chunk<T>::unpack(v, f);
+#pragma unroll
+    for (int q = 0; q < Chunk<T>::N; ++q) x = q == k ? f[q] : x;
+    return x;
+}
 
 // Long rows: a block takes LG_CHUNKS chunks of 16 bytes of one row.  Chunks that two rows share are written by both, element by
 // element.  2048 x 50,000 bf16 by the kernel below, which divides to find a chunk's row: 173 us; by this one 67 us (6.1 TB/s).
 constexpr int LG_PER = 4, LG_CHUNKS = 256 * LG_PER;
 
-template <typename T>
+template <typename T, bool REST>
 __global__ void __launch_bounds__(256)
 log_probs_backward_rows_kernel(const LpGradParams P, int parts) {
     pdl_wait();
@@ -776,7 +813,7 @@ log_probs_backward_rows_kernel(const LpGradParams P, int parts) {
     const int64_t c0 = e0 / PER + (int64_t)(blockIdx.x % parts) * LG_CHUNKS + threadIdx.x;
     const T* const z = (const T*)P.z;
     T* const dz = (T*)P.dz;
-    LpRow R;
+    LpRow<REST> R;
     R.read(P, row);
     const int64_t hit = R.y >= 0 && R.y < P.C ? e0 + R.y : -1;
     uint4 v[LG_PER];
@@ -784,6 +821,11 @@ log_probs_backward_rows_kernel(const LpGradParams P, int parts) {
     for (int u = 0; u < LG_PER; ++u) {
         const int64_t i = c0 + u * 256;
         if (i < c1 && (i + 1) * PER <= all) v[u] = ld_16(z + i * PER);
+    }
+    float share = R.g;
+    if constexpr (REST) {  // by the thread that writes the label
+        const int64_t q = hit / PER - c0;
+        if (hit >= 0 && q >= 0 && q < LG_CHUNKS && q % 256 == 0) share = R.at_label((float)z[hit]);
     }
 #pragma unroll
     for (int u = 0; u < LG_PER; ++u) {
@@ -797,20 +839,20 @@ log_probs_backward_rows_kernel(const LpGradParams P, int parts) {
             if (hit >= i * PER && hit < (i + 1) * PER) {
 #pragma unroll
                 for (int k = 0; k < PER; ++k)
-                    if (hit == i * PER + k) f[k] += R.g;
+                    if (hit == i * PER + k) f[k] = REST ? share : f[k] + share;
             }
             *reinterpret_cast<uint4*>(dz + i * PER) = Chunk<T>::pack(f);
         } else {
             for (int k = 0; k < PER; ++k) {
                 const int64_t e = i * PER + k;
-                if (e >= e0 && e < e1) dz[e] = T(R((float)z[e]) + (e == hit ? R.g : 0.f));
+                if (e >= e0 && e < e1) dz[e] = T(REST && e == hit ? share : R((float)z[e]) + (e == hit ? share : 0.f));
             }
         }
     }
 }
 
 // short rows: a chunk of 16 bytes per thread and step, whatever rows its elements lie in
-template <typename T, typename I>
+template <typename T, typename I, bool REST>
 __global__ void __launch_bounds__(256)
 log_probs_backward_kernel(const LpGradParams P) {
     pdl_wait();
@@ -819,20 +861,42 @@ log_probs_backward_kernel(const LpGradParams P) {
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
         const bool whole = (i + 1) * PER <= all;
         float f[PER];
-        if (whole) Chunk<T>::unpack(ld_16((const T*)P.z + i * PER), f);
-        else
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (whole) {
+            raw = ld_16((const T*)P.z + i * PER);
+            Chunk<T>::unpack(raw, f);
+        } else {
 #pragma unroll
             for (int k = 0; k < PER; ++k) f[k] = i * PER + k < all ? (float)((const T*)P.z)[i * PER + k] : 0.f;
+            if constexpr (REST) raw = Chunk<T>::pack(f);  // (exact)
+        }
         int64_t row = (I)(i * PER) / (I)P.C;
         int c = (int)(i * PER - row * P.C);
-        LpRow R;
+        LpRow<REST> R;
         R.read(P, row);
+        uint32_t labels = 0;  // (REST: expm1 once per label, not once per element: 170k x 47 fp32 29 -> 27 us)
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            f[k] = R(f[k]) + (c == R.y ? R.g : 0.f);
+            if constexpr (REST) {
+                f[k] = R(f[k]);
+                if (c == R.y) labels |= 1u << k;
+            } else {
+                f[k] = R(f[k]) + (c == R.y ? R.g : 0.f);
+            }
             if (++c == P.C) {
                 c = 0;
                 if (++row < P.N && k + 1 < PER) R.read(P, row);
+            }
+        }
+        if constexpr (REST) {
+            while (labels) {
+                const int at = __ffs(labels) - 1;
+                labels &= labels - 1;
+                R.read(P, (I)(i * PER + at) / (I)P.C);
+                const float v = R.at_label(lp_pick<T>(raw, at));
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (k == at) f[k] = v;
             }
         }
         if (whole) *reinterpret_cast<uint4*>((T*)P.dz + i * PER) = Chunk<T>::pack(f);
@@ -902,6 +966,11 @@ size_t gnn_log_probs_workspace(int32_t N, int C, int top, gnn_dtype dtype) {
 
 gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, gnn_dtype dtype, int top, float* logp, float* entropy, float* lse,
                          float* top_logp, int32_t* top_idx, void* ws, size_t ws_bytes, gnn_stream stream) {
+    return gnn_log_probs_rest(Z, label, N, C, dtype, top, logp, entropy, lse, nullptr, top_logp, top_idx, ws, ws_bytes, stream);
+}
+
+gnn_status gnn_log_probs_rest(const void* Z, const int32_t* label, int32_t N, int C, gnn_dtype dtype, int top, float* logp, float* entropy, float* lse,
+                              float* lse_rest, float* top_logp, int32_t* top_idx, void* ws, size_t ws_bytes, gnn_stream stream) {
     const char* who = "gnn_log_probs";
     GNN_REQUIRE(N >= 0 && C > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
     GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
@@ -916,7 +985,7 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
     cudaStream_t st = as_stream(stream);
     LpParams P;
     P.z = Z; P.label = label; P.N = N; P.C = C; P.top = top;
-    P.logp = logp; P.entropy = entropy; P.lse = lse; P.top_logp = top_logp; P.top_idx = top_idx;
+    P.logp = logp; P.entropy = entropy; P.lse = lse; P.lse_rest = lse_rest; P.top_logp = top_logp; P.top_idx = top_idx;
     P.parts = (int)lw.parts; P.stats = (float*)ws; P.keys = (uint64_t*)((char*)ws + lw.keys);
     const bool f32 = dtype == GNN_F32;
     const int64_t chunks = (int64_t)C / (f32 ? 4 : 8) + 2;  // of a row, both ends cut
@@ -958,6 +1027,11 @@ gnn_status gnn_log_probs(const void* Z, const int32_t* label, int32_t N, int C, 
 
 gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                                   int32_t N, int C, gnn_dtype dtype, void* dZ, gnn_stream stream) {
+    return gnn_log_probs_rest_backward(Z, label, lse, nullptr, entropy, dlogp, dentropy, N, C, dtype, dZ, stream);
+}
+
+gnn_status gnn_log_probs_rest_backward(const void* Z, const int32_t* label, const float* lse, const float* lse_rest, const float* entropy, const float* dlogp,
+                                       const float* dentropy, int32_t N, int C, gnn_dtype dtype, void* dZ, gnn_stream stream) {
     const char* who = "gnn_log_probs_backward";
     GNN_REQUIRE(N >= 0 && C > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
     GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
@@ -968,19 +1042,23 @@ gnn_status gnn_log_probs_backward(const void* Z, const int32_t* label, const flo
     GNN_REQUIRE(aligned16(Z) && aligned16(dZ), GNN_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
     cudaStream_t st = as_stream(stream);
     LpGradParams P;
-    P.z = Z; P.label = label; P.N = N; P.C = C; P.lse = lse; P.entropy = entropy; P.dlogp = dlogp; P.dentropy = dentropy; P.dz = dZ;
+    P.z = Z; P.label = label; P.N = N; P.C = C; P.lse = lse; P.lse_rest = lse_rest; P.entropy = entropy; P.dlogp = dlogp; P.dentropy = dentropy; P.dz = dZ;
     const int per = dtype == GNN_F32 ? 4 : 8;
     const int64_t parts = ceil_div((int64_t)C / per + 2, LG_CHUNKS), blocks = parts * N;
-    if (C >= 2048 && blocks <= INT32_MAX) {
-        if (dtype == GNN_F32) launch_overlapped(log_probs_backward_rows_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
-        else launch_overlapped(log_probs_backward_rows_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
-    } else {
+    const bool narrow = (int64_t)N * C + 8 <= UINT32_MAX;  // the division that finds a chunk's row
+    auto run = [&](auto t, auto rest) {
+        using T = decltype(t);
+        constexpr bool REST = decltype(rest)::value;
+        if (C >= 2048 && blocks <= INT32_MAX) {
+            launch_overlapped(log_probs_backward_rows_kernel<T, REST>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
+            return;
+        }
         const dim3 grid((unsigned)grid_for(ceil_div((int64_t)N * C, per), 256));
-        auto run = [&](auto kernel) { launch_overlapped(kernel, grid, dim3(256), 0, st, P); };
-        const bool narrow = (int64_t)N * C + 8 <= UINT32_MAX;  // the division that finds a chunk's row
-        if (dtype == GNN_F32) narrow ? run(log_probs_backward_kernel<float, uint32_t>) : run(log_probs_backward_kernel<float, int64_t>);
-        else narrow ? run(log_probs_backward_kernel<__nv_bfloat16, uint32_t>) : run(log_probs_backward_kernel<__nv_bfloat16, int64_t>);
-    }
+        if (narrow) launch_overlapped(log_probs_backward_kernel<T, uint32_t, REST>, grid, dim3(256), 0, st, P);
+        else launch_overlapped(log_probs_backward_kernel<T, int64_t, REST>, grid, dim3(256), 0, st, P);
+    };
+    if (dtype == GNN_F32) lse_rest ? run(float(), std::true_type()) : run(float(), std::false_type());
+    else lse_rest ? run(__nv_bfloat16(), std::true_type()) : run(__nv_bfloat16(), std::false_type());
     GNN_CHECK_LAUNCH(who);
     return GNN_OK;
 }

@@ -128,6 +128,8 @@ SIGNATURES = {
     "gnn_log_probs_workspace": (_SZ, [_I32, _INT, _INT, _INT]),
     "gnn_log_probs": (_INT, [_VP, _VP, _I32, _INT, _INT, _INT, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
     "gnn_log_probs_backward": (_INT, [_VP, _VP, _VP, _VP, _VP, _VP, _I32, _INT, _INT, _VP, _VP]),
+    "gnn_log_probs_rest": (_INT, [_VP, _VP, _I32, _INT, _INT, _INT, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
+    "gnn_log_probs_rest_backward": (_INT, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _INT, _INT, _VP, _VP]),
     "gnn_propagate_fused_host": (_INT, [_CSR, _INT, _INT, _VP, _VP, _INT, _INT, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
     "gnn_propagate_fused_backward_host": (_INT, [_CSR, _INT, _INT, _VP, _VP, _VP, _INT, _INT, _VP, _VP, _VP, _VP, _SZ, _VP]),
 }
@@ -468,10 +470,12 @@ def linear_i8(xq, x_scale, wq, w_scale, bias=None, relu=False, dtype=torch.float
     return _b.linear_i8(xq, x_scale, wq, w_scale, bias, relu, dtype == torch.bfloat16, ws, return_ws)
 
 
-def log_probs(Z, label=None, top=0, want_entropy=True, ws=None):
-    """-> (logp [N] or None, entropy [N] or None, lse [N], top_logp [N,top], top_idx [N,top])"""
-    return _b.log_probs(Z, label, top, want_entropy, ws)
+def log_probs(Z, label=None, top=0, want_entropy=True, ws=None, return_rest=False):
+    """-> (logp [N] or None, entropy [N] or None, lse [N], top_logp [N,top], top_idx [N,top]); with return_rest also lse_rest [N],
+    what the rounding of lse leaves out: give it to log_probs_backward wherever scores may be large or rows nearly sure."""
+    return _b.log_probs(Z, label, top, want_entropy, ws, return_rest)
 
 
-def log_probs_backward(Z, label, lse, dlogp=None, entropy=None, dentropy=None):
-    return _b.log_probs_backward(Z, label, lse, dlogp, entropy, dentropy)
+def log_probs_backward(Z, label, lse, dlogp=None, entropy=None, dentropy=None, lse_rest=None):
+    """-> dZ.  Without lse_rest (log_probs' return_rest) every p is off by half a unit of lse's last bit, as in exp(Z - lse)."""
+    return _b.log_probs_backward(Z, label, lse, dlogp, entropy, dentropy, lse_rest)
