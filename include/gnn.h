@@ -536,7 +536,8 @@ gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, i
 /* Y[i,m] = act( x_scale[i] * w_scale[m] * sum_k xq[i,k] * wq[m,k] + bias[m] ): gnn_linear_bias_act for answering, with
  * features and weights in 8 bits.  xq int8 [N,K], wq int8 [M,K] (a row per output channel), both 16-byte aligned, x_scale
  * float [N], w_scale float [M], bias float [M] or NULL, Y [N,M] of dtype, 16-byte aligned.  The sums are exact (int32; K up
- * to 131071, GNN_ERR_UNSUPPORTED beyond); scales, bias and relu in fp32, one rounding to dtype.
+ * to 131071, GNN_ERR_UNSUPPORTED beyond); in fp32 the sum, its product with x_scale, and w_scale and bias in one rounding
+ * more (no product on the way overflows where the result does not), relu, then the rounding to dtype.
  * ws: gnn_linear_i8_workspace(N, K, M) bytes, asked for the sizes of each call, 16-byte aligned; its first 4 bytes are the
  * status word of gnn_linear. */
 size_t gnn_linear_i8_workspace(int32_t N, int K, int M);

@@ -249,7 +249,8 @@ linear_i8_rows_kernel(const int8_t* xq, const float* sx, const int8_t* wq, const
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (lane != r || n0 + r >= N) continue;
-        float y = fmaf((float)acc[r] * sx[n0 + r], sw[m], bias ? bias[m] : 0.f);  // as the tensor-core path rounds
+        const float s = sx[n0 + r], b = bias ? bias[m] : 0.f;
+        float y = sg_i8_wide(s) ? sg_i8_wide_value(acc[r], s, sw[m], b) : sg_i8_value(acc[r], s, sw[m], b);  // as the tensor-core path rounds
         if (relu) y = y < 0.f ? 0.f : y;
         Y[(int64_t)(n0 + r) * M + m] = T(y);
     }

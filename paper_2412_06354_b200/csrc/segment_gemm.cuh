@@ -334,6 +334,16 @@ __device__ __forceinline__ void sg_zero_outside(const SegGemmParams& P, T* out) 
     for (int64_t i = p1 + me; i < end; i += all) out[i] = T(0.f);
 }
 
+// SG_I8: sum * sx * sw + b, roundings of the sum, of its product with sx, of the result.  A sum is under 2^31: from |sx| of 2^96 on (rows of
+// 1e31 and more) that product may pass the largest number where the result does not; there 2^-32 of it meets 2^32 sw, in which a
+// scale that has no room for that becomes the largest number (the result has none either, unless the sum is 0).  The same digits.
+__device__ __forceinline__ bool sg_i8_wide(float sx) { return fabsf(sx) > 0x1p96f; }
+__device__ __forceinline__ float sg_i8_value(int sum, float sx, float sw, float b) { return fmaf((float)sum * sx, sw, b); }
+__device__ __forceinline__ float sg_i8_wide_value(int sum, float sx, float sw, float b) {
+    const float w = fabsf(sw) > 0x1p95f && fabsf(sw) < INFINITY ? copysignf(3.402823466e38f, sw) : sw * 0x1p32f;
+    return fmaf((float)sum * (sx * 0x1p-32f), w, b);
+}
+
 // a chunk of 16 bytes, not under floor: 0 (relu) or -inf, twice as bf16; a NaN stays.  (Of rounded values, as of the sums.)
 __device__ __forceinline__ uint4 sg_pack(const float* f, const float*, uint32_t floor) {
     float g[4] = {f[0], f[1], f[2], f[3]};
@@ -556,7 +566,7 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                         const float4 w = *reinterpret_cast<const float4*>(&s_cols[1][c]), b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
                         const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) f[q] = fmaf((float)(int)r[q] * sx, wv[q], bv[q]);  // (zeros where there is no bias)
+                        for (int q = 0; q < 4; ++q) f[q] = sg_i8_value((int)r[q], sx, wv[q], bv[q]);  // (zeros where there is no bias)
                     } else if constexpr (MODE == SG_Y) {
                         const float4 b = *reinterpret_cast<const float4*>(&s_cols[0][c]);
                         f[0] = __uint_as_float(r[0]) + b.x; f[1] = __uint_as_float(r[1]) + b.y; f[2] = __uint_as_float(r[2]) + b.z; f[3] = __uint_as_float(r[3]) + b.w;
@@ -602,6 +612,27 @@ segment_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
                     }
                 } else {
                     send((T*)P.out + row0 * P.cols_out, P.cols_out, P.vec != 0, P.bulk != 0, (int)row0);
+                    // rare: such rows once more, element by element, behind their stores (asked before send, where the scale has just been
+                    // loaded, 170k x 256 -> 256 took 1 us longer; as a choice for each sum 5 us)
+                    if (MODE == SG_I8 && __any_sync(0xFFFFFFFFu, sg_i8_wide(sx))) {
+                        sg_stores_done(lane);
+                        __syncwarp();
+                        T* const out = (T*)P.out + (row0 + lane) * P.cols_out + c_base;
+                        constexpr int WIDE = 64 / sizeof(T), EVERY = SG_EPI_WARPS / 4;  // the columns that this warp has stored, 16 at a time
+                        for (int i = 0;; ++i) {
+                            const int c0 = (sub + i / (WIDE / 16) * EVERY) * WIDE + i % (WIDE / 16) * 16;
+                            if (c0 >= bn || c_base + c0 >= c_end) break;
+                            uint32_t r[16];
+                            tmem_ld16(taddr + (uint32_t)c0, r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) {
+                                float v = sg_i8_wide_value((int)r[q], sx, s_cols[MODE == SG_I8 ? 1 : 0][c0 + q], s_cols[0][c0 + q]);
+                                asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(__uint_as_float(floor & 0xFFFF0000u)));
+                                if (sg_i8_wide(sx) && lane < rows && c_base + c0 + q < c_end) out[c0 + q] = T(v);
+                            }
+                        }
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
