@@ -326,7 +326,10 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     GNN_REQUIRE(ws && ws_bytes >= iw.bytes, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed", who, iw.bytes);
     cudaStream_t st = as_stream(stream);
     const bool few = i8_few_rows(N);
-    if (N == 0) return GNN_OK;
+    if (N == 0) {
+        if (cudaMemsetAsync(ws, 0, sizeof(int), st) != cudaSuccess) GNN_FAIL(GNN_ERR_CUDA, "%s: memset failed (is it a device pointer?)", who);
+        return GNN_OK;
+    }
     GNN_REQUIRE(xq && x_scale && wq && w_scale && Y, GNN_ERR_INVALID_ARG, "%s: null argument", who);
     GNN_REQUIRE(aligned16(xq) && aligned16(wq) && aligned16(Y) && aligned16(ws), GNN_ERR_INVALID_ARG, "%s: matrices and workspace must be 16-byte aligned", who);
     if (few) {
