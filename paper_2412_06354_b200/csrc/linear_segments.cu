@@ -124,10 +124,11 @@ static int apart(int cols, gnn_dtype dtype) { return dtype == GNN_F32 ? (cols + 
 
 // How the rows are cut for dW: parts x tiles blocks of work on 148 SMs.  Few parts mean few partials; as many as keep the SMs
 // busy: the smallest number whose last wave costs at most 5 % over the best of all numbers, parts of at least 256 rows.  And of
-// at most 4096 (bf16: 65536) rows: every 16 rows the accumulator loses up to one unit of its 24th bit, so that a sum of terms
-// of one sign is off by 4096 / 16 * 2^-24 = 1.5e-5 of its value at most, half that on average (bf16: 2^-12, under the rounding).
+// at most 2048 rows in fp32, as the forward product's contraction: every 16 rows the accumulator cuts off what lies under the last bit of a
+// 24-bit sum, measured up to 0.9 * 2^-24 of the result (terms of one sign made for it: 1.35e-5 over 4096 rows, 6.8e-6 over 2048; others half of
+// that).  bf16: 65536 rows, 2^-12, under the rounding.
 static int64_t dw_parts(int64_t N, int64_t tiles, bool f32) {
-    const int64_t longest = f32 ? 4096 : 65536, least = N > longest ? ceil_div(N, longest) : 1;
+    const int64_t longest = f32 ? 2048 : 65536, least = N > longest ? ceil_div(N, longest) : 1;
     int64_t most = N / 256;
     if (most > 296) most = 296;
     if (most < least) most = least;
