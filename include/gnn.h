@@ -503,9 +503,11 @@ gnn_status gnn_linear_backward(const void* X, const void* W, const void* dY, int
  * seg_ptr[g] .. seg_ptr[g+1]-1, the form that gnn_graph_ptr_from_ids gives (int64 [G+1] on the device, non-decreasing,
  * 0 <= seg_ptr[0], seg_ptr[G] <= N; read on the device only).  Segments may be empty; rows of no segment (before seg_ptr[0],
  * from seg_ptr[G] on) become 0.  X [N,K], W [G,K,M], Y [N,M] of dtype, bias float [G,M] or NULL; relu != 0: max(., 0)
- * before the single rounding (a NaN stays).  K and M: any up to 8192 (fp32: 2048; GNN_ERR_UNSUPPORTED beyond), G K < 2^31.
+ * before the single rounding (a NaN stays).  K and M: any up to 8192 (fp32: 2048), G up to 2^24, G K < 2^31, N up to 2^31 - 130
+ * (GNN_ERR_UNSUPPORTED beyond).
  * Matrices and ws are 16-byte aligned.  Tensor cores with fp32 accumulation: bf16 directly, fp32 by an exact three-term bf16
- * split as in gnn_linear (a value that is not finite, or whose magnitude is above 3.38e38, gives NaN in the results it enters).
+ * split as in gnn_linear (a value that is not finite, or whose magnitude is above 3.38e38, gives NaN in the results it enters; one below 1e-34
+ * is taken to within 2^-134, which is all that bf16 numbers hold).
  * A seg_ptr that descends gives unspecified results; every access stays inside the arguments.
  * Rows of one segment only ever meet their own weight: what another segment holds (infinities, NaN) does not reach them.
  * ws: gnn_linear_segments_workspace(..., backward = 0) bytes, asked for the sizes of each call; it holds copies of bf16
@@ -536,7 +538,7 @@ gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, i
 /* Y[i,m] = act( x_scale[i] * w_scale[m] * sum_k xq[i,k] * wq[m,k] + bias[m] ): gnn_linear_bias_act for answering, with
  * features and weights in 8 bits.  xq int8 [N,K], wq int8 [M,K] (a row per output channel), both 16-byte aligned, x_scale
  * float [N], w_scale float [M], bias float [M] or NULL, Y [N,M] of dtype, 16-byte aligned.  The sums are exact (int32; K up
- * to 131071, GNN_ERR_UNSUPPORTED beyond); in fp32 the sum, its product with x_scale, and w_scale and bias in one rounding
+ * to 131071, N up to 2^31 - 130, GNN_ERR_UNSUPPORTED beyond); in fp32 the sum, its product with x_scale, and w_scale and bias in one rounding
  * more (no product on the way overflows where the result does not), relu, then the rounding to dtype.
  * ws: gnn_linear_i8_workspace(N, K, M) bytes, asked for the sizes of each call, 16-byte aligned; its first 4 bytes are the
  * status word of gnn_linear. */

@@ -7,8 +7,9 @@
 // t = sum of exp(z - m) (z - m).  Then lse = m + log1p(s) and H = log1p(s) - t / (1 + s): without the leading 1 in the sum, a
 // row whose best class is nearly sure keeps the digits of its small log p and entropy.  Two parts are joined by scaling the one
 // with the smaller maximum, whose own maximum counts again: exp(m1 - m2) (s1 + 1).
-// The k best: keys of (score, lower index first) that are all different, sorted over the lanes of a warp; a chunk whose largest
-// score does not pass the worst of them is left alone.
+// The k best: keys of (score, lower index first) that are all different.  A floor of the k-th best, from the threads' largest scores, leaves
+// few chunks to look at again, and what reaches it in them is sorted over the lanes of a warp; where too few or too many do, every class is
+// offered to a sorted list (log_probs_kernel).  Rows of few classes: log_probs_few_kernel.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -18,7 +19,10 @@
 namespace gnn {
 
 constexpr int LP_TOP = 32;            // classes listed at most: a lane each
-constexpr int LP_WARP_CLASSES = 1024;  // rows up to here by a warp
+// Rows up to here by a warp, longer ones by a block.  By a warp / by a block, fp32, no list: 20,000 rows of 300 classes 13.5 / 66 us, of 1000 19.9 / 71, of
+// 2000 39 / 90; five best 30 / 112, 68 / 117, 93 / 143; but 64 rows of 1000, five best: 11.0 / 4.1.  (Many rows would gain from a
+// higher border, few rows from a lower one.)
+constexpr int LP_WARP_CLASSES = 1024;
 constexpr int LP_SLOT = 56;           // of allow_big_smem: four of them
 constexpr int LP_CLUSTER = 8;         // parts of a row that a cluster of blocks joins; more leave theirs in the workspace
 
@@ -31,13 +35,6 @@ __device__ __forceinline__ float lp_exp(float d) {  // exp of d <= 0: 2^(d log2 
 struct LpStats {
     float m, s, t;
     __device__ __forceinline__ void clear() { m = -INFINITY; s = 0.f; t = 0.f; }
-    // the maximum becomes v > m
-    __device__ __forceinline__ void raise(float v) {
-        const float d = m - v, f = lp_exp(d), c = f * (s + 1.f);  // m = -inf: f = 0
-        t = fmaf(fmaxf(d, -1000.f), c, f * t);
-        s = c;
-        m = v;
-    }
     // z <= m, or not a number (which then shows in s)
     __device__ __forceinline__ void add(float z, float base) {
         const float d = z - base, e = lp_exp(d);
@@ -433,8 +430,8 @@ log_probs_kernel(const LpParams P) {
     if (row >= P.N) return;  // (W = 1: a whole warp; no block-wide step follows)
     const T* const z = (const T*)P.z;
     // 16-byte chunks of the whole matrix that hold elements of the row (of the part): the row's first and last may hold others' too
-    const int64_t e0 = row * P.C, e1 = e0 + P.C, all = P.N * P.C;
-    int64_t c0 = e0 / PER, c1 = (e1 + PER - 1) / PER;
+    const int64_t e0 = row * P.C, all = P.N * P.C;
+    int64_t c0 = e0 / PER, c1 = (e0 + P.C + PER - 1) / PER;
     if (P.parts > 1) {
         const int64_t per = (c1 - c0 + P.parts - 1) / P.parts, n0 = c0 + part * per, n1 = n0 + per;
         c1 = n1 < c1 ? n1 : c1;
@@ -799,8 +796,11 @@ __device__ __forceinline__ float lp_pick(uint4 v, int k) {
     return x;
 }
 
-// Long rows: a block takes LG_CHUNKS chunks of 16 bytes of one row.  Chunks that two rows share are written by both, element by
-// element.  2048 x 50,000 bf16 by the kernel below, which divides to find a chunk's row: 173 us; by this one 67 us (6.1 TB/s).
+// Long rows, from LG_CLASSES on: a block takes LG_CHUNKS chunks of 16 bytes of one row.  Chunks that two rows share are written by both, element
+// by element.  2048 x 50,000 bf16 67 us (6.1 TB/s).  This kernel / the one below, which divides to find a chunk's row, 20,000 rows: 349 classes fp32
+// 31 / 13 us, bf16 36 / 11; 1000 classes 42 / 46, 36 / 26; 2000 classes 58 / 86, 47 / 59; 4000 classes 95 / 160, 64 / 110.  (fp32 would gain from
+// a border of 1000.)
+constexpr int LG_CLASSES = 2048;
 constexpr int LG_PER = 4, LG_CHUNKS = 256 * LG_PER;
 
 template <typename T, bool REST>
@@ -921,8 +921,9 @@ static int64_t lp_parts(int64_t N, int64_t C, int s) {
     return best;
 }
 
-// a thread per row: few classes, and rows enough to fill the SMs with threads
-static bool lp_few(int64_t N, int C, int top) { return C <= LP_FEW && N >= 4096; }
+// A thread per row: few classes, and rows enough to fill the SMs with threads.  By a thread / by a warp, fp32, five best: 170,000 x 47 12.3 / 158 us, 16,384 x 64
+// 7.3 / 17.0, 4096 x 64 6.1 / 6.0, 2048 x 64 6.0 / 5.5, 256 x 64 5.9 / 4.1.  (Up to 16 classes a thread is the faster one from 256 rows on: 3.6 / 4.2.)
+static bool lp_few(int64_t N, int C) { return C <= LP_FEW && N >= 4096; }
 
 // launch_overlapped with clusters
 template <class... Params, class... Args>
@@ -989,7 +990,7 @@ gnn_status gnn_log_probs_rest(const void* Z, const int32_t* label, int32_t N, in
     P.parts = (int)lw.parts; P.stats = (float*)ws; P.keys = (uint64_t*)((char*)ws + lw.keys);
     const bool f32 = dtype == GNN_F32;
     const int64_t chunks = (int64_t)C / (f32 ? 4 : 8) + 2;  // of a row, both ends cut
-    if (lp_few(N, C, top)) {
+    if (lp_few(N, C)) {
         const dim3 grid((unsigned)ceil_div(N, LP_ROWS));
         const size_t smem = ((size_t)LP_ROWS * lp_few_stride(C) + 8) * 4;
         auto run = [&](auto kernel) { launch_overlapped(kernel, grid, dim3(LP_ROWS), smem, st, P); };
@@ -1049,7 +1050,7 @@ gnn_status gnn_log_probs_rest_backward(const void* Z, const int32_t* label, cons
     auto run = [&](auto t, auto rest) {
         using T = decltype(t);
         constexpr bool REST = decltype(rest)::value;
-        if (C >= 2048 && blocks <= INT32_MAX) {
+        if (C >= LG_CLASSES && blocks <= INT32_MAX) {
             launch_overlapped(log_probs_backward_rows_kernel<T, REST>, dim3((unsigned)blocks), dim3(256), 0, st, P, (int)parts);
             return;
         }

@@ -678,7 +678,10 @@ inline int sg_block(int cols, int most, int64_t row_tiles) {
 
 // How the tiles of SG_Y, SG_DX and SG_I8 are dealt out (see above).  Pairs: where the weights of a tile are too many to stay, contractions of
 // eight slices and a tile of 256 rows for every SM (65,536 x 1024 -> 1024 over 64 segments: 144 us in ones, 138 in pairs, both with stores by the warps).
-// Otherwise ranges where all weights together are a fraction of L2 and the rows give every SM a few tiles.
+// In pairs / in ones, short runs: 65,536 rows of 4 types 512 x 1024 73 / 94 us, 1024 x 1024 119 / 150, 768 x 768 79 / 88; 40,000 rows of 8 types 512 x 512 29.6 / 29.1.
+// Otherwise ranges where all weights together are a fraction of L2 and the rows give every SM a few tiles.  Ranges / tiles dealt out, 128 x 128 bf16: 38,000
+// rows of 4 types 9.1 / 9.8 us, 170,000 rows of 12 types 18.1 / 24.4, of 330 22.3 / 30.5; fewer tiles than that: 30,000 rows 8.1 / 8.1, 10,000 7.6 / 7.1;
+// weights over 32 MB make no difference (100,000 rows of 190 types 512 x 256: 45 / 45).  (700 types, 243 rows each: 25.0 / 31.0, where the rule deals out.)
 inline bool sg_stays(const SegGemmParams& P) { return SG_EPI_WARPS * SG_STAGING + (size_t)P.bn * 128 * P.slices + 4 * SG_A_BYTES <= SG_SMEM_MAX; }
 inline void sg_deal(SegGemmParams& P, size_t weight_bytes, bool pairs = true) {
     const int64_t row_tiles = P.N / TC_ROWS + P.G;
