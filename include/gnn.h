@@ -531,7 +531,7 @@ gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, c
 /* Rows to 8 bits: scale[i] = max_k |X[i,k]| / 127 (fp32, one rounding), q[i,k] = X[i,k] / scale[i] rounded to the nearest
  * integer, ties to even, as the exact quotient would be (127 at most: a subnormal scale may have been rounded down).  A row of
  * zeros has scale 0 and zeros; a row with a value that is not finite has scale NaN and zeros, so that what is computed from it
- * is NaN.  X [N,K] of dtype, q int8 [N,K] (both 16-byte aligned), scale float [N].  Weights [K,M] are transposed first: a row of
+ * is NaN.  X [N,K] of dtype, q int8 [N,K] (both 16-byte aligned), scale float [N]; K up to 2^31 - 257 (GNN_ERR_UNSUPPORTED beyond).  Weights [K,M] are transposed first: a row of
  * q is an output channel. */
 gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, int8_t* q, float* scale, gnn_stream stream);
 

@@ -303,6 +303,7 @@ gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, i
     const char* who = "gnn_quantize_rows";
     GNN_REQUIRE(N >= 0 && K > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
     GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
+    GNN_REQUIRE(K <= INT32_MAX - 256, GNN_ERR_UNSUPPORTED, "%s: K up to 2^31 - 257", who);  // a step of 256 behind the last stays an int
     if (N == 0) return GNN_OK;
     GNN_REQUIRE(X && q && scale, GNN_ERR_INVALID_ARG, "%s: null argument", who);
     GNN_REQUIRE(aligned16(X) && aligned16(q), GNN_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
