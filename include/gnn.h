@@ -531,14 +531,14 @@ gnn_status gnn_linear_segments_backward(const void* X, const int64_t* seg_ptr, c
 /* Rows to 8 bits: scale[i] = max_k |X[i,k]| / 127 (fp32, one rounding), q[i,k] = X[i,k] / scale[i] rounded to the nearest
  * integer, ties to even, as the exact quotient would be (127 at most: a subnormal scale may have been rounded down).  A row of
  * zeros has scale 0 and zeros; a row with a value that is not finite has scale NaN and zeros, so that what is computed from it
- * is NaN.  X [N,K] of dtype, q int8 [N,K] (both 16-byte aligned), scale float [N]; K up to 2^31 - 257 (GNN_ERR_UNSUPPORTED beyond).  Weights [K,M] are transposed first: a row of
- * q is an output channel. */
+ * is NaN.  X [N,K] of dtype, q int8 [N,K] (both 16-byte aligned), scale float [N]; K up to 2^31 - 257 (GNN_ERR_UNSUPPORTED
+ * beyond).  Weights [K,M] are transposed first: a row of q is an output channel. */
 gnn_status gnn_quantize_rows(const void* X, int32_t N, int K, gnn_dtype dtype, int8_t* q, float* scale, gnn_stream stream);
 
 /* Y[i,m] = act( x_scale[i] * w_scale[m] * sum_k xq[i,k] * wq[m,k] + bias[m] ): gnn_linear_bias_act for answering, with
  * features and weights in 8 bits.  xq int8 [N,K], wq int8 [M,K] (a row per output channel), both 16-byte aligned, x_scale
  * float [N], w_scale float [M], bias float [M] or NULL, Y [N,M] of dtype, 16-byte aligned.  The sums are exact (int32; K up
- * to 131071, N up to 2^31 - 130, GNN_ERR_UNSUPPORTED beyond); in fp32 the sum, its product with x_scale, and w_scale and bias in one rounding
+ * to 131071, N up to 2^31 - 130, M up to 2^31 - 257, GNN_ERR_UNSUPPORTED beyond); in fp32 the sum, its product with x_scale, and w_scale and bias in one rounding
  * more (no product on the way overflows where the result does not), relu, then the rounding to dtype.
  * ws: gnn_linear_i8_workspace(N, K, M) bytes, asked for the sizes of each call, 16-byte aligned; its first 4 bytes are the
  * status word of gnn_linear. */

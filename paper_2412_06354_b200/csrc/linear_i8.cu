@@ -324,7 +324,7 @@ gnn_status gnn_linear_i8(const int8_t* xq, const float* x_scale, const int8_t* w
     GNN_REQUIRE(N >= 0 && K > 0 && M > 0, GNN_ERR_INVALID_ARG, "%s: bad shape", who);
     GNN_REQUIRE(dtype == GNN_F32 || dtype == GNN_BF16, GNN_ERR_INVALID_ARG, "%s: bad dtype", who);
     // 128 * 128 * K stays inside int32
-    GNN_REQUIRE(K <= 131071 && N < INT32_MAX - TC_ROWS, GNN_ERR_UNSUPPORTED, "%s: K up to 131071", who);
+    GNN_REQUIRE(K <= 131071 && N < INT32_MAX - TC_ROWS && M <= INT32_MAX - 256, GNN_ERR_UNSUPPORTED, "%s: K up to 131071, N up to 2^31 - 130, M up to 2^31 - 257", who);
     const I8Ws iw(N, K, M);
     GNN_REQUIRE(ws && ws_bytes >= iw.bytes, GNN_ERR_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed", who, iw.bytes);
     cudaStream_t st = as_stream(stream);
