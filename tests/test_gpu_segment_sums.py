@@ -29,3 +29,24 @@ def test_longest_parts(gnn, N, K, M):
         _, dW = gnn.linear_segments_backward(X, ptr, W, (a * scale).expand(N, M).contiguous().cuda(), want_dX=False)
         ref = float((a.double() * a.double() * scale).sum())
         assert float((dW.double() - ref).abs().max()) <= 1e-5 * ref, scale
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-34, 1e-36, 1e-38, 1e-40])
+def test_smallest_values(gnn, size):
+    """fp32 values of which the second and third bf16 term have few bits or none: within 2^-134 of each value, beside the sums' 1e-5."""
+    import torch
+    g = torch.Generator().manual_seed(1)
+    X, W, dY = torch.randn(300, 72, generator=g) * size, torch.randn(2, 72, 40, generator=g), torch.randn(300, 40, generator=g) * size
+    ptr = torch.tensor([0, 130, 300])
+    Xd, Wd, pd = X.cuda(), W.cuda(), ptr.cuda()
+    Y = gnn.linear_segments(Xd, pd, Wd).double().cpu()
+    dX, _ = gnn.linear_segments_backward(None, pd, Wd, dY.cuda(), want_dW=False)
+    Z = torch.randn(300, 40, generator=g)
+    _, dW = gnn.linear_segments_backward(Xd, pd, Wd, Z.cuda(), want_dX=False)
+    for s in range(2):
+        r = slice(int(ptr[s]), int(ptr[s + 1]))
+        for got, a, b in ((Y[r], X[r], W[s]), (dX[r].double().cpu(), dY[r], W[s].t()), (dW[s].double().cpu(), X[r].t(), Z[r])):
+            a, b = a.double(), b.double()
+            # and products of either factor's terms under the smallest fp32 number, 2^-149 of each at most
+            room = 1e-5 * (a.abs() @ b.abs()) + 2.0 ** -134 * b.abs().sum(0) + a.shape[1] * 6 * 2.0 ** -149
+            assert bool(((got - a @ b).abs() <= room).all()), float(((got - a @ b).abs() / room).max())
