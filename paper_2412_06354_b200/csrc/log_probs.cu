@@ -232,8 +232,8 @@ __device__ __forceinline__ void lp_finish(const LpParams& P, int64_t row, const 
 // over through shared memory, as they lie (words of a warp's rows then fall on one bank at most two at a time), or, where the
 // number of classes is a multiple of four, in rows of an odd number of 16-byte words.
 // The best: the largest of the groups' largest scores (eight classes each), then its group again in shared memory, where what is
-// taken becomes NaN.  170,000 x 47, five best: by a warp per row 241 us, with a row's scores in registers, looked through for every
-// class listed, 29 us; so 15.6 us (2.1 TB/s; half of all cycles issue).
+// taken becomes NaN.  170,000 x 47, five best: by a warp per row 158 us, with a row's scores in registers, looked through for every
+// class listed, 29 us; so 15.8 us (2.1 TB/s; half of all cycles issue).
 constexpr int LP_ROWS = 128;  // of a block
 constexpr int LP_FEW = 64;    // classes at most: NG groups of eight
 __host__ __device__ constexpr int lp_few_stride(int C) { return C % 4 == 0 ? (C / 4 | 1) * 4 : C; }
@@ -407,7 +407,8 @@ __device__ __forceinline__ float lp_chunk_max(uint4 v) {
 // threads' own largest scores is a floor of the k-th best class; only chunks that reach it are looked at again (in L1 or L2),
 // about k of thousands, and what reaches it in them is sorted.  Where that gives fewer than k classes or more than LP_CAND (many
 // equal scores, rows masked nearly throughout, scores that are not numbers) the classes are offered to a sorted list one by
-// one.  256 x 170,000 bf16, ten best: 31 us, 175 us with all offered one by one.  Chunks
+// one.  256 x 170,000 bf16, ten best: 31 us, 175 us with all offered one by one, 113 us where scores spread evenly over 8 to 16 have
+// thousands of equals at the top.  Chunks
 // fetched a step ahead, through shared memory or registers, other numbers of parts, or a maximum of which the sums follow only every
 // e^2: 33 to 44 us; a part's results pushed to the first block instead of fetched by it: 34 us.
 constexpr int LP_CAND = 256;

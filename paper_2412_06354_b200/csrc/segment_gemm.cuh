@@ -36,9 +36,10 @@
 //   warps 2-17 epilogue: accumulator -> registers -> swizzled staging -> rows of 64 bytes to global memory, rows and columns that
 //              do not exist left out.  (Eight warps with 128 bytes: 8-bit product of 170,000 x 256 -> 256 40 us, of which 20 without
 //              any epilogue; sixteen 32 us, and 29 with the bulk stores below.)
-// Measured: 170,000 x 128 -> 128 over 12 segments 18 us (4.8 TB/s: HBM, and 4 us of start and end), 65,536 x 1024 -> 1024 over 64 133 us
-// (1.03 PFLOP/s: copies from L2), gradients of 100,000 x 256 x 256 over 12 58 us, 8 bits 170,000 x 256 -> 256 to bf16 29 us (4.5 TB/s),
-// 16,384 x 2048 -> 2048 to fp32 65 us (2.1e15 operations a second).
+// Measured in short runs (in runs of seconds, under the power cap): 170,000 x 128 -> 128 over 12 segments 18.5 us (20.5; 4.7 TB/s: HBM, and 4 us of start
+// and end), 65,536 x 1024 -> 1024 over 64 134 us (157; 1.02 and 0.88 PFLOP/s: copies from L2), gradients of 100,000 x 256 x 256 over 12 58 us (62),
+// 8 bits 170,000 x 256 -> 256 to bf16 29 us (4.5 TB/s), 16,384 x 2048 -> 2048 to fp32 65.5 us (2.1e15 operations a second; with the rounding of its
+// rows 96, 109 in long runs).
 // fp32 (segment_gemm_f32_kernel): the same pieces of work, every value as three bf16 terms.
 //
 // Every wait has an iteration limit, as in linear_tma.cu.
