@@ -197,3 +197,30 @@ def test_guard_bands(guarded, dtype, n, C):  # noqa: F811
     d = torch.ones(n, device="cuda")
     gnn.log_probs_backward(Z, y, lse.clone(), dlogp=d, entropy=H.clone(), dentropy=d, lse_rest=rest.clone())
     gt.check("gradient")
+
+
+def test_last_layer_with_scores_far_from_zero(gnn):
+    """Typed last layer -> log probabilities -> their gradient -> the layer's gradients, with a bias that moves a type's scores by thousands:
+    each step against 64 bits from the step before, and rows of the gradient that add up to nothing."""
+    import torch
+    g = torch.Generator().manual_seed(21)
+    ptr = torch.tensor([0, 700, 700, 1500])
+    X, W = torch.randn(1500, 64, generator=g), torch.randn(3, 64, 47, generator=g) * 0.3
+    b = torch.tensor([0.0, 5.0, -3000.0])[:, None] + torch.randn(3, 47, generator=g)
+    label = torch.randint(-1, 47, (1500,), generator=g, dtype=torch.int32)
+    Xd, Wd, pd, y = X.cuda(), W.cuda(), ptr.cuda(), label.cuda()
+    Z = gnn.linear_segments(Xd, pd, Wd, bias=b.cuda())
+    logp, H, lse, _, _, rest = gnn.log_probs(Z, y, return_rest=True)
+    dl, dh = torch.full((1500,), -1.0), torch.full((1500,), -0.01)
+    dZ = gnn.log_probs_backward(Z, y, lse, dlogp=dl.cuda(), entropy=H, dentropy=dh.cuda(), lse_rest=rest)
+    ref, lp, size = reference(Z.cpu(), label, dl, dh)
+    room = 2.0 * (4e-6 + 2.0 ** -22 * lp.abs()) * size + 2.0 ** -22 * ref.abs() + 1e-38
+    near(dZ, ref, room, "dZ")
+    assert bool((dZ.double().sum(1).abs().cpu() <= room.sum(1)).all())
+    dX, dW = gnn.linear_segments_backward(Xd, pd, Wd, dZ)
+    d = dZ.double().cpu()
+    for s in range(3):
+        r = slice(int(ptr[s]), int(ptr[s + 1]))
+        x, w = X[r].double(), W[s].double()
+        near(dX[r], d[r] @ w.t(), 1e-5 * (d[r].abs() @ w.abs().t()), "dX")
+        near(dW[s], x.t() @ d[r], 1e-5 * (x.t().abs() @ d[r].abs()), "dW")
